@@ -568,6 +568,105 @@ int ef_measure_peak(ef_ctx *ctx, int what, const void *buf, size_t bytes, int re
 /* Fake-copy contexts only: advance the fake clock; copies complete after bytes/bandwidth seconds. */
 int ef_fake_advance_time(ef_ctx *ctx, double seconds);
 
+/* -------------------------------------------------------------------------------------------------
+ * Operators beside the layer: routing from logits, and products of 8-bit codes (cite no passage of the
+ * paper).  They take no context: shapes come with the call, scratch is the caller's (`work`, 16-byte aligned
+ * device memory of at least the number of bytes the *_work function gives; calls that may overlap in time
+ * need scratch of their own), and ef_last_error(NULL) has the text of the calling thread's last failure.
+ * They only enqueue kernels on `stream`: no allocation, no synchronisation, no host copy, so all of them may
+ * be captured into a graph.  Every sum has a fixed order: equal inputs give equal bits.
+ * ------------------------------------------------------------------------------------------------- */
+enum { EF_BF16 = 0, EF_F16 = 1, EF_F32 = 2, EF_I8 = 3 };          /* element types */
+enum { EF_SCORE_SOFTMAX = 0, EF_SCORE_SIGMOID = 1 };
+
+#define EF_ROUTER_MAX_EXPERTS 512
+#define EF_ROUTER_MAX_TOPK 16
+#define EF_ROUTER_MAX_GROUPS 32
+
+typedef struct ef_router {
+    int32_t n_experts;    /* E, 1..EF_ROUTER_MAX_EXPERTS */
+    int32_t top_k;        /* k, 1..EF_ROUTER_MAX_TOPK, at most the experts of groups_kept groups */
+    int32_t score;        /* EF_SCORE_* */
+    int32_t n_groups;     /* groups of E / n_groups neighbouring experts; divides E; 1 = no groups */
+    int32_t groups_kept;  /* 1..n_groups */
+    int32_t group_best;   /* a group's value: 1 = its best choice value, 2 = the sum of its two best (groups of two and more) */
+    int32_t renorm;       /* 1: the k weights of a token are divided by their sum */
+    float scale;          /* factor on the weights */
+} ef_router;
+
+/*
+ * Routing of T tokens from their logits z [T, E]: score s = softmax(z) over all E or sigmoid(z); choice value
+ * c = s + bias (bias [E] f32 or NULL; it chooses and never weighs).  With groups, the groups_kept groups of the
+ * highest value stay (ties: lower group), the experts of the others are out.  ids = the k experts of the highest
+ * c (ties: lower expert), ascending; w = s[ids], over their sum if renorm, times scale.  Then the stable grouping
+ * of the assignments a = t*k + j by expert, as ef_route: counts, offsets, perm, inv_perm.
+ * Comparisons are those of the scores' real values: s and c are formed in 32 bits, and again in 64 where the
+ * border of a choice lies within the error of 32.  A logit of -inf or NaN has score 0 and choice value -inf (its
+ * expert comes after every other of its token); a bias of NaN counts as -inf; logits of +inf share a softmax
+ * evenly.  A token whose scores are all 0 has weights 0, and its ids by the same rules.
+ *   logits [dev] T rows of E elements of `type` (EF_BF16, EF_F16, EF_F32), ld elements from row to row
+ *   topk_ids [T,k] i32, topk_w [T,k] f32, counts [E] i32, offsets [E+1] i32, perm, inv_perm [T*k] i32  [dev]
+ * T = 0 is allowed (counts and offsets are zeroed); T*k below 2^31.
+ */
+size_t ef_route_scores_work(const ef_router *r, int T);   /* 0 if r or T is out of range */
+int ef_route_scores(const ef_router *r, const void *logits, int type, int64_t ld, const float *bias, int T,
+                    int32_t *topk_ids, float *topk_w, int32_t *counts, int32_t *offsets, int32_t *perm,
+                    int32_t *inv_perm, void *work, size_t work_bytes, void *stream);
+
+/*
+ * Rows to 8 bits with a scale each: scale = max(f32(max|x| / 127), 2^-126); code = x / scale rounded to the
+ * nearest whole number (ties to even; the quotient itself, not a product with a reciprocal), so codes are in
+ * -127..127.  A row that holds an infinity or a NaN gets codes 0 and a scale of NaN: what is computed from it is NaN.
+ * Quantises activations (a row = a token) and weights [N, K] (a row = an output channel) alike.
+ *   x [dev] rows of K elements of `type` (EF_BF16, EF_F16, EF_F32), ldx elements from row to row;
+ *   codes [dev] i8, ldc bytes from row to row, the bytes from K up to the next multiple of 64, as far as ldc
+ *   reaches, are zeroed; scales [dev] [rows] f32.  rows = 0 is allowed.
+ */
+int ef_quant_rows(const void *x, int type, int64_t ldx, int rows, int K, int8_t *codes, int64_t ldc, float *scales,
+                  void *stream);
+
+/*
+ * Products of 8-bit codes with a scale for every token and every output channel, for one matrix or for the
+ * experts of a layer:
+ *   y[i][n] = a_scale[r] * w_scale[g][n] * sum_k a[r][k] * w[g][n][k],
+ * g the group of product row i (offsets[g] <= i < offsets[g+1]), r = rows[i] / row_div its row of `a`
+ * (rows == NULL: r = i).  The sum is in whole numbers and exact.  With swiglu the rows of a matrix are F gate rows
+ * and then F up rows (N = 2F), and out[i][f] = silu(y[i][f]) * y[i][F+f]; otherwise out = y.  Rounded once, to out_type.
+ * Values beyond EF_F16's range become infinite.
+ * `a` of 16 or 32 bits is quantised in the call as ef_quant_rows does (all a_rows rows, once).
+ * Rows outside all groups are not written.  Offsets outside 0..M or descending, and row numbers outside `a`, are
+ * caught on the device: an offset is clamped (one that lies before an earlier one counts as that one), a row of `a`
+ * that does not exist counts as NaN.
+ */
+typedef struct ef_q8_product {
+    const void *a;            /* [dev] a_rows rows of K elements of a_type, lda elements from row to row */
+    const float *a_scale;     /* [dev] [a_rows] f32, for EF_I8; NULL otherwise */
+    const int32_t *rows;      /* [dev] [M] or NULL (then M <= a_rows) */
+    const int32_t *offsets;   /* [dev] [G+1] or NULL (G = 1: all M rows) */
+    const void *w;            /* [dev] i8, 16-byte aligned: G matrices of N rows of K codes, ldw bytes from row to row,
+                                 w_group bytes from matrix to matrix, both multiples of 16, ldw >= K rounded up to 16
+                                 (every matrix holds N whole rows of that many readable bytes) */
+    const float *w_scale;     /* [dev] [G,N] f32 */
+    void *out;                /* [dev] M rows of N (swiglu: N/2) elements of out_type, ldo elements from row to row */
+    int64_t lda, ldw, w_group, ldo;
+    int32_t a_type;           /* EF_I8, EF_BF16, EF_F16, EF_F32 */
+    int32_t out_type;         /* EF_BF16, EF_F16, EF_F32 */
+    int32_t a_rows, M, N, K, G;   /* K <= 131071; G <= EF_ROUTER_MAX_EXPERTS; M = 0 is allowed */
+    int32_t row_div;          /* >= 1 (perm of ef_route: top_k) */
+    int32_t swiglu;           /* 0/1; N even */
+} ef_q8_product;
+size_t ef_matmul_q8_work(const ef_q8_product *p);   /* bytes of scratch; depends on the shape fields and types only */
+int ef_matmul_q8(const ef_q8_product *p, void *work, size_t work_bytes, void *stream);
+
+/*
+ * Weighted sum of the expert rows of each token, the last step of a layer made of the calls above:
+ * out[t] = sum_j w[t][j] * y[inv_perm[t*k+j]], j ascending, in 32 bits, rounded once.  inv_perm == NULL: the
+ * identity.  A row number outside 0..y_rows-1 counts as a row of NaN.
+ *   y [dev] y_rows rows of d elements of y_type, ldy from row to row; out [dev] [T] rows of d, ldo from row to row
+ */
+int ef_combine(const void *y, int y_type, int64_t ldy, int y_rows, const float *w, const int32_t *inv_perm, int T, int k,
+               int d, void *out, int out_type, int64_t ldo, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

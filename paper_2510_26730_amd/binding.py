@@ -36,7 +36,11 @@ EXPORTS = [
     "ef_delta_cache_create", "ef_delta_cache_destroy", "ef_delta_cache_put", "ef_delta_cache_get",
     "ef_delta_cache_counts", "ef_delta_producer_create", "ef_delta_producer_destroy", "ef_delta_submit",
     "ef_delta_drain", "ef_delta_assemble",
+    "ef_route_scores_work", "ef_route_scores", "ef_quant_rows", "ef_matmul_q8_work", "ef_matmul_q8", "ef_combine",
 ]
+EF_BF16, EF_F16, EF_F32, EF_I8 = 0, 1, 2, 3
+EF_SCORE_SOFTMAX, EF_SCORE_SIGMOID = 0, 1
+EF_ROUTER_MAX_EXPERTS, EF_ROUTER_MAX_TOPK, EF_ROUTER_MAX_GROUPS = 512, 16, 32
 
 
 class ef_config(C.Structure):
@@ -85,6 +89,18 @@ class ef_tuning(C.Structure):
 class ef_forest_config(C.Structure):
     _fields_ = [("n_features", C.c_int32), ("n_outputs", C.c_int32), ("n_trees", C.c_int32),
                 ("max_depth", C.c_int32), ("min_samples_leaf", C.c_int32), ("n_threads", C.c_int32)]
+
+
+class ef_router(C.Structure):
+    _fields_ = [("n_experts", C.c_int32), ("top_k", C.c_int32), ("score", C.c_int32), ("n_groups", C.c_int32),
+                ("groups_kept", C.c_int32), ("group_best", C.c_int32), ("renorm", C.c_int32), ("scale", C.c_float)]
+
+
+class ef_q8_product(C.Structure):
+    _fields_ = [("a", C.c_void_p), ("a_scale", C.c_void_p), ("rows", C.c_void_p), ("offsets", C.c_void_p), ("w", C.c_void_p),
+                ("w_scale", C.c_void_p), ("out", C.c_void_p), ("lda", C.c_int64), ("ldw", C.c_int64), ("w_group", C.c_int64),
+                ("ldo", C.c_int64), ("a_type", C.c_int32), ("out_type", C.c_int32), ("a_rows", C.c_int32), ("M", C.c_int32),
+                ("N", C.c_int32), ("K", C.c_int32), ("G", C.c_int32), ("row_div", C.c_int32), ("swiglu", C.c_int32)]
 
 
 class EfError(RuntimeError):
@@ -156,6 +172,15 @@ def lib():
         L.ef_delta_producer_destroy.argtypes = [vp]
         L.ef_delta_submit.argtypes = [vp, vp, i32, i32, i32, i32, vp]
         L.ef_delta_drain.argtypes = [vp]
+        i64, szt = C.c_int64, C.c_size_t
+        L.ef_route_scores_work.restype = szt
+        L.ef_route_scores_work.argtypes = [vp, i32]
+        L.ef_route_scores.argtypes = [vp, vp, i32, i64, vp, i32, vp, vp, vp, vp, vp, vp, vp, szt, vp]
+        L.ef_quant_rows.argtypes = [vp, i32, i64, i32, i32, vp, i64, vp, vp]
+        L.ef_matmul_q8_work.restype = szt
+        L.ef_matmul_q8_work.argtypes = [vp]
+        L.ef_matmul_q8.argtypes = [vp, vp, szt, vp]
+        L.ef_combine.argtypes = [vp, i32, i64, i32, vp, vp, i32, i32, i32, vp, i32, i64, vp]
         L.ef_delta_assemble.argtypes = [vp, vp, vp, i32, i32, i32, i32, i32, f32, vp, C.POINTER(i32)]
         _lib = L
     return _lib
@@ -545,3 +570,99 @@ def ef_delta_assemble(c, token_ids, tok_off, layer, S, H, L, gain, M, out=None):
     _rc(lib().ef_delta_assemble(c, _ptr(tok), _ptr(off), R, layer, S, H, L, gain, _ptr(delta), C.byref(hits)),
         "ef_delta_assemble")
     return delta, hits.value
+
+
+# ---- operators beside the layer ------------------------------------------------------------------
+# Two-dimensional operands may have any row stride; their elements of a row are consecutive.
+
+def _rows(x):
+    """(address, type, elements from row to row) of a matrix of tensor rows."""
+    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise EfError(EF_EINVAL, "a matrix with consecutive row elements is needed")
+    name = str(x.dtype)
+    kind = {"torch.bfloat16": EF_BF16, "torch.float16": EF_F16, "torch.float32": EF_F32, "torch.int8": EF_I8}.get(name)
+    if kind is None:
+        raise EfError(EF_EINVAL, f"unsupported element type {name}")
+    return x.data_ptr(), kind, x.stride(0) if x.shape[0] > 1 else max(x.stride(0), x.shape[1])
+
+
+def _work(work):
+    return (None, 0) if work is None else (_ptr(work), work.numel() * work.element_size())
+
+
+def _router(E, k, sigmoid, n_groups, groups_kept, group_best, renorm, scale):
+    return ef_router(E, k, EF_SCORE_SIGMOID if sigmoid else EF_SCORE_SOFTMAX, n_groups, groups_kept, group_best, int(renorm), scale)
+
+
+def ef_route_scores_work(T, E, k, n_groups=1, groups_kept=1):
+    """Bytes of scratch of ef_route_scores; 0 if a size is out of range."""
+    return int(lib().ef_route_scores_work(C.byref(_router(E, k, False, n_groups, groups_kept, 1, False, 1.0)), T))
+
+
+def ef_route_scores(logits, bias, ids, w, counts, offsets, perm, inv_perm, work, *, sigmoid=False, n_groups=1, groups_kept=1,
+                    group_best=1, renorm=False, scale=1.0, stream=None):
+    """Routing of logits [T, E]: ids, w [T, k]; counts [E], offsets [E+1], perm, inv_perm [T*k] of the stable grouping."""
+    z, kind, ld = _rows(logits)
+    T, E = logits.shape
+    r = _router(E, ids.shape[1], sigmoid, n_groups, groups_kept, group_best, renorm, scale)
+    wp, wb = _work(work)
+    return _check(None, lib().ef_route_scores(C.byref(r), z, kind, ld, _ptr(bias), T, _ptr(ids), _ptr(w), _ptr(counts), _ptr(offsets),
+                                              _ptr(perm), _ptr(inv_perm), wp, wb, _stream(stream)))
+
+
+def ef_quant_rows(x, codes, scales, stream=None):
+    """Rows of x [rows, K] to int8 codes [rows, >= K] (zeroed up to the next multiple of 64 columns) and scales [rows]."""
+    xp, kind, ldx = _rows(x)
+    cp, ckind, ldc = _rows(codes)
+    if ckind != EF_I8 or codes.shape[0] != x.shape[0] or codes.shape[1] < x.shape[1]:
+        raise EfError(EF_EINVAL, "ef_quant_rows: codes must be int8 and as large as x")
+    if scales.numel() < x.shape[0]:
+        raise EfError(EF_EINVAL, "ef_quant_rows: a scale for every row is needed")
+    return _check(None, lib().ef_quant_rows(xp, kind, ldx, x.shape[0], x.shape[1], cp, min(ldc, max(codes.shape[1], x.shape[1])) if x.shape[0] == 1 else ldc,
+                                            _ptr(scales), _stream(stream)))
+
+
+def _product(a, w, w_scale, out, a_scale, rows, row_div, offsets, swiglu):
+    p = ef_q8_product()
+    p.a, p.a_type, p.lda = _rows(a)
+    p.out, p.out_type, p.ldo = _rows(out)
+    if str(w.dtype) != "torch.int8" or w.dim() not in (2, 3) or (w.shape[-1] > 1 and w.stride(-1) != 1):
+        raise EfError(EF_EINVAL, "ef_matmul_q8: w must be int8 [N, K] or [G, N, K] with consecutive row elements")
+    p.G, (p.N, p.K) = (w.shape[0] if w.dim() == 3 else 1), w.shape[-2:]
+    p.w, p.ldw = w.data_ptr(), w.stride(-2) if p.N > 1 else (p.K + 15) // 16 * 16
+    p.w_group = w.stride(0) if p.G > 1 else 0
+    cols = p.N // 2 if swiglu else p.N
+    if a.shape[1] < p.K or (p.a_type != EF_I8 and a.shape[1] != p.K):
+        raise EfError(EF_EINVAL, f"ef_matmul_q8: rows of {a.shape[1]} against K = {p.K}")
+    p.a_rows, p.M = a.shape[0], out.shape[0]
+    if (out.shape[1] != cols or w_scale.numel() != p.G * p.N or (rows is not None and rows.numel() < p.M)
+            or (offsets is not None and offsets.numel() != p.G + 1) or (a_scale is not None and a_scale.numel() < p.a_rows)):
+        raise EfError(EF_EINVAL, "ef_matmul_q8: out, scales, rows or offsets do not fit the product")
+    p.a_scale, p.rows, p.offsets, p.w_scale = _ptr(a_scale), _ptr(rows), _ptr(offsets), _ptr(w_scale)
+    p.row_div, p.swiglu = row_div, int(swiglu)
+    return p
+
+
+def ef_matmul_q8_work(a, w, w_scale, out, *, a_scale=None, rows=None, row_div=1, offsets=None, swiglu=False):
+    """Bytes of scratch of ef_matmul_q8 with the same arguments."""
+    return int(lib().ef_matmul_q8_work(C.byref(_product(a, w, w_scale, out, a_scale, rows, row_div, offsets, swiglu))))
+
+
+def ef_matmul_q8(a, w, w_scale, out, work=None, *, a_scale=None, rows=None, row_div=1, offsets=None, swiglu=False, stream=None):
+    """out = a_scale * w_scale * (a w^T) with 8-bit codes: `a` [R, K] of codes (with a_scale [R]) or of floats that the call
+    quantises, w int8 [N, K] or [G, N, K] with scales [G, N], out [M, N] (swiglu: [M, N/2]).  offsets [G+1]: product rows of
+    each matrix; rows [M]: row of `a` (after division by row_div) of each product row."""
+    p = _product(a, w, w_scale, out, a_scale, rows, row_div, offsets, swiglu)
+    wp, wb = _work(work)
+    return _check(None, lib().ef_matmul_q8(C.byref(p), wp, wb, _stream(stream)))
+
+
+def ef_combine(y, w, inv_perm, out, stream=None):
+    """out[t] = sum_j w[t, j] * y[inv_perm[t*k + j]]; w [T, k] f32, inv_perm [T*k] i32 or None (rows in order)."""
+    yp, ykind, ldy = _rows(y)
+    op, okind, ldo = _rows(out)
+    T, k = w.shape
+    if out.shape[0] != T or out.shape[1] != y.shape[1] or (inv_perm is not None and inv_perm.numel() != T * k):
+        raise EfError(EF_EINVAL, "ef_combine: shapes do not fit")
+    return _check(None, lib().ef_combine(yp, ykind, ldy, y.shape[0], _ptr(w), _ptr(inv_perm), T, k, y.shape[1], op, okind, ldo,
+                                         _stream(stream)))

@@ -1,0 +1,77 @@
+// Launch interface between the context-free operators' entry points (ef_ops.hip) and their kernels
+// (ef_router.hip, ef_q8.hip).
+#pragma once
+#include "../../include/expertflow.h"
+
+#include <hip/hip_runtime.h>
+#include <cstdint>
+
+namespace ef {
+
+// ---- routing from logits (ef_router.hip) -------------------------------------------------------
+constexpr int kRouterWaves = 16;        // waves of a workgroup; one token per wave at a time
+
+struct RouterArgs {
+    ef_router r;
+    const void *logits;
+    int type;
+    long long ld;
+    const float *bias;
+    int T;
+    int32_t *ids;
+    float *w;
+    int32_t *counts, *offsets, *perm, *inv_perm;
+    int ntiles;            // token tiles of router_tile(T) tokens
+    int32_t *tile_counts;  // [E][ntiles] (scratch): assignments of a tile to an expert, then their prefixes over the tiles
+    uint8_t *rank;         // [T*k] (scratch): earlier tokens of the tile with the same expert
+};
+int router_tile(int T);
+hipError_t launch_router(const RouterArgs &a, hipStream_t s);
+
+// ---- 8-bit products (ef_q8.hip) ----------------------------------------------------------------
+struct QuantArgs {
+    const void *x;
+    int type;
+    long long ldx;
+    int rows, K;
+    int8_t *codes;
+    long long ldc;
+    float *scales;         // null: x are codes already, only padded
+};
+hipError_t launch_quant_rows(const QuantArgs &a, hipStream_t s);
+
+// `a` as codes whose rows are zero from K up to the next multiple of 64
+struct Q8Args {
+    const int8_t *a;
+    long long lda;
+    const float *a_scale;
+    int a_rows;
+    const int32_t *rows;
+    int row_div, M;
+    const int32_t *offsets;
+    int G;
+    const int8_t *w;
+    long long ldw, w_group;
+    const float *w_scale;
+    int N, K, swiglu;
+    void *out;
+    int out_type;
+    long long ldo;
+};
+hipError_t launch_q8_product(const Q8Args &a, hipStream_t s);
+
+struct CombineArgs {
+    const void *y;
+    int y_type;
+    long long ldy;
+    int y_rows;
+    const float *w;
+    const int32_t *inv_perm;
+    int T, k, d;
+    void *out;
+    int out_type;
+    long long ldo;
+};
+hipError_t launch_combine_rows(const CombineArgs &a, hipStream_t s);
+
+}  // namespace ef

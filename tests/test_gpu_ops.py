@@ -1,0 +1,455 @@
+"""The operators beside the layer on the device, against the plain 64-bit implementations of oracle/ops.py.
+
+Whole numbers have to be equal.  Tolerances of the others count roundings: 2^-24 relative for each in 32 bits, half a step of the
+output type at the end."""
+import numpy as np
+import pytest
+import torch
+
+import oracle.ops as ops
+from paper_2510_26730_amd import binding as ef
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TYPES = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}
+
+
+def half_step(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def stream():
+    return torch.cuda.current_stream()
+
+
+def near(got, want, tol, what):
+    got = f64(got)
+    assert got.shape == want.shape, what
+    assert np.array_equal(np.isnan(got), np.isnan(want)), what
+    off = np.abs(np.nan_to_num(got) - np.nan_to_num(want))
+    worst = np.max(off / np.maximum(np.nan_to_num(tol), 1e-300)) if off.size else 0
+    print(f"{what}: {worst:.3f} of the tolerance", flush=True)
+    assert worst <= 1, what
+
+
+# ---- routing ------------------------------------------------------------------------------------
+
+def run_route(z, bias, k, dtype=torch.float32, pad=0, **kw):
+    """z: torch matrix on the host -> the call's outputs, with `pad` unused columns behind each row of logits."""
+    T, E = z.shape
+    wide = torch.full((T, E + pad), float("nan"), dtype=dtype, device="cuda")
+    wide[:, :E] = z.to(dtype)
+    i32 = lambda n: torch.full((n + 8,), -7, dtype=torch.int32, device="cuda")  # noqa: E731
+    o = dict(ids=i32(T * k), counts=i32(E), offsets=i32(E + 1), perm=i32(T * k), inv_perm=i32(T * k),
+             w=torch.full((T * k + 8,), -7.0, device="cuda"))
+    size = ef.ef_route_scores_work(T, E, k, kw.get("n_groups", 1), kw.get("groups_kept", 1))
+    assert size > 0
+    work = torch.full((size + 64,), 0xA5, dtype=torch.uint8, device="cuda")
+    ef.ef_route_scores(wide[:, :E], None if bias is None else bias.cuda(), o["ids"][:T * k].view(T, k), o["w"][:T * k].view(T, k),
+                       o["counts"][:E], o["offsets"][:E + 1], o["perm"][:T * k], o["inv_perm"][:T * k], work[:size], stream=stream(), **kw)
+    torch.cuda.synchronize()
+    for v in o.values():
+        assert (v[-8:] == -7).all()
+    assert (work[size:] == 0xA5).all()
+    n = dict(ids=T * k, w=T * k, counts=E, offsets=E + 1, perm=T * k, inv_perm=T * k)
+    return {name: v[:n[name]].cpu().numpy() for name, v in o.items()}, f64(wide[:, :E])
+
+
+def check_route(z, bias, k, dtype=torch.float32, pad=0, **kw):
+    got, zd = run_route(z, bias, k, dtype, pad, **kw)
+    want = ops.route_scores(zd, None if bias is None else f64(bias), k, **kw)
+    for name in ("ids", "counts", "offsets", "perm", "inv_perm"):
+        assert np.array_equal(got[name], want[name].reshape(-1)), name
+    fin = zd[np.isfinite(zd)]
+    # exponent's rounding, exp, sums over the wave and over the chosen, quotients, scale
+    tol = want["w"] * (np.ptp(fin) if fin.size else 0) * U + want["w"] * 40 * U + 1e-37
+    near(torch.from_numpy(got["w"]).view(-1, k), want["w"], tol, f"route {tuple(z.shape)} k={k} {kw}")
+
+
+ROUTES = [
+    # T, E, k, type, extras
+    (1, 64, 6, "f32", {}), (1, 1, 1, "f32", {}), (3, 8, 2, "bf16", dict(renorm=True)), (16, 60, 4, "f16", {}),
+    (63, 64, 8, "f32", dict(sigmoid=True)), (64, 65, 8, "bf16", dict(renorm=True)), (65, 128, 8, "f32", dict(sigmoid=True, renorm=True)),
+    (17, 256, 8, "f32", dict(sigmoid=True, n_groups=8, groups_kept=4, group_best=2, renorm=True, scale=2.5)),
+    (100, 257, 16, "f32", dict(scale=16.0)), (33, 512, 16, "bf16", dict(n_groups=32, groups_kept=5, group_best=2)),
+    (129, 160, 6, "f32", dict(n_groups=8, groups_kept=3, scale=16.0)), (70, 6, 2, "f32", dict(n_groups=3, groups_kept=1, group_best=2)),
+    (1000, 60, 4, "bf16", dict(renorm=True)), (9000, 128, 6, "f16", dict(sigmoid=True, n_groups=4, groups_kept=2)),
+    (70, 512, 16, "f32", dict(n_groups=2, groups_kept=1)), (40, 34, 3, "f32", dict(n_groups=17, groups_kept=2, group_best=2, sigmoid=True)),
+    (8193, 8, 2, "f32", dict(renorm=True)),
+]
+
+
+@pytest.mark.parametrize("with_bias", [False, True])
+@pytest.mark.parametrize("T,E,k,dtype,kw", ROUTES, ids=[f"{r[0]}-{r[1]}-{r[2]}-{r[3]}-{i}" for i, r in enumerate(ROUTES)])
+def test_route(T, E, k, dtype, kw, with_bias):
+    gen = torch.Generator().manual_seed(T * 1000 + E)
+    z = 2 * torch.randn(T, E, generator=gen)
+    bias = 0.1 * torch.randn(E, generator=gen) if with_bias else None
+    check_route(z, bias, k, TYPES[dtype], pad=T % 3, **kw)
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(sigmoid=True), dict(sigmoid=True, n_groups=4, groups_kept=2, group_best=2), dict(n_groups=4, groups_kept=2)])
+@pytest.mark.parametrize("with_bias", [False, True])
+def test_route_ties_go_to_the_lowest(kw, with_bias):
+    """Few distinct logits, and biases of few distinct values: nearly every border is a tie."""
+    gen = torch.Generator().manual_seed(5)
+    z = torch.randint(-2, 3, (200, 96), generator=gen).float()
+    z[0] = 0.0
+    z[1, ::2] = -0.0
+    z[1, 1::2] = 0.0
+    bias = torch.randint(0, 2, (96,), generator=gen).float() / 4 if with_bias else None
+    check_route(z, bias, 5, **kw)
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(n_groups=8, groups_kept=3, group_best=2)])
+def test_route_borders_closer_than_32_bits(kw):
+    """Scores that 32 bits cannot tell apart: sigmoids of large logits, biases that make up for their scores to the last bit."""
+    gen = torch.Generator().manual_seed(6)
+    z = 15 + 3 * torch.rand(300, 64, generator=gen)
+    check_route(z, None, 4, sigmoid=True, **kw)
+    z = torch.randn(1, 64, generator=gen).expand(300, 64).contiguous()
+    bias = -torch.sigmoid(z[0].double()).float()
+    check_route(z, bias, 4, sigmoid=True, **kw)
+    check_route(z + 1e-4 * torch.randn(300, 64, generator=gen), bias, 4, sigmoid=True, **kw)
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("with_bias", [False, True])
+@pytest.mark.parametrize("groups", [dict(), dict(n_groups=4, groups_kept=2, group_best=2), dict(n_groups=4, groups_kept=2)])
+def test_route_masked_logits(sigmoid, dtype, with_bias, groups):
+    """-inf, NaN, +inf, the type's lowest value; rows that leave nothing or fewer than k."""
+    gen = torch.Generator().manual_seed(7)
+    z = torch.randn(40, 48, generator=gen)
+    inf, nan, low = float("inf"), float("nan"), torch.finfo(TYPES[dtype]).min
+    z[0] = -inf
+    z[1] = nan
+    z[2] = low
+    z[3, :] = -inf
+    z[3, 40] = 1.0
+    z[4, ::2] = nan
+    z[5, :46] = -inf
+    z[6, 7] = inf
+    z[7, 3:9] = inf
+    z[8, :] = low
+    z[8, 20] = -inf
+    z[9] = torch.where(torch.arange(48) % 3 == 0, z[9], torch.tensor(low))
+    z[10:20][torch.rand(10, 48, generator=gen) < 0.9] = -inf
+    bias = None
+    if with_bias:
+        bias = 0.3 * torch.randn(48, generator=gen)
+        bias[5], bias[17] = -inf, nan
+    check_route(z, bias, 4, TYPES[dtype], sigmoid=sigmoid, renorm=True, **groups)
+
+
+def test_route_of_no_tokens():
+    z = torch.empty(0, 12, device="cuda")
+    i32 = lambda *n: torch.full(n, -1, dtype=torch.int32, device="cuda")  # noqa: E731
+    counts, offsets = i32(12), i32(13)
+    ef.ef_route_scores(z, None, i32(0, 2), torch.empty(0, 2, device="cuda"), counts, offsets, i32(0), i32(0), None, stream=stream())
+    assert (counts == 0).all() and (offsets == 0).all()
+
+
+# ---- rows to 8 bits ------------------------------------------------------------------------------
+
+def check_quant(x, pad_x=0, pad_c=0):
+    """x on the host, already of its type."""
+    rows, K = x.shape
+    wide = torch.full((rows, K + pad_x), float("nan"), dtype=x.dtype, device="cuda")
+    wide[:, :K] = x
+    room = (K + 63) // 64 * 64
+    codes = torch.full((rows, K + pad_c), 99, dtype=torch.int8, device="cuda")
+    scales = torch.full((rows + 4,), -1.0, device="cuda")
+    ef.ef_quant_rows(wide[:, :K], codes, scales[:rows], stream=stream())
+    torch.cuda.synchronize()
+    q, s = ops.quant_rows(f64(x))
+    assert np.array_equal(codes[:, :K].cpu().numpy(), q)
+    assert np.array_equal(f64(scales[:rows]), s, equal_nan=True)
+    assert (codes[:, K:room] == 0).all() and (codes[:, room:] == 99).all() and (scales[rows:] == -1).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows,K,pad_x,pad_c", [(1, 1, 0, 0), (1, 64, 0, 0), (3, 63, 0, 1), (5, 65, 1, 100), (2, 1000, 8, 24), (7, 2048, 0, 0),
+                                                (3, 4097, 3, 200), (2, 14336, 0, 64), (1, 40000, 0, 0), (300, 24, 0, 40), (9, 1408, 8, 16)])
+def test_quant_rows(dtype, rows, K, pad_x, pad_c):
+    gen = torch.Generator().manual_seed(rows * 100 + K)
+    check_quant((torch.randn(rows, K, generator=gen) * torch.logspace(-6, 3, rows)[:, None]).to(TYPES[dtype]), pad_x, pad_c)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_quant_rows_at_the_halves(dtype):
+    """Rows in which many quotients are halves or next to halves, rows of zeros, subnormals, the type's largest and lowest."""
+    t = TYPES[dtype]
+    rows = []
+    for amax in (127.0, 254.0, 1.0, 0.75, 1.984375, 31.75, 3.0):
+        n = torch.arange(-127, 128).double()
+        s = np.float64(np.float32(amax / 127))
+        rows += [torch.cat([n * s * 0.5, torch.tensor([amax, -amax / 2, amax / 2]).double()]).to(t), torch.cat([(n + 0.5) * s, torch.tensor([amax] * 3).double()]).clamp(-amax, amax).to(t)]
+        up = torch.cat([(n + 0.5) * s, torch.tensor([amax] * 3).double()]).clamp(-amax, amax)
+        rows += [(up * (1 + 2.0 ** -22)).clamp(-amax, amax).to(t), (up * (1 - 2.0 ** -22)).to(t)]
+    small = torch.finfo(t).tiny
+    rows += [torch.zeros(258).to(t), torch.full((258,), small).to(t), (torch.arange(258) * small / 64).to(t)]
+    rows += [torch.full((258,), torch.finfo(t).max).to(t), torch.full((258,), torch.finfo(t).min).to(t)]
+    check_quant(torch.stack(rows))
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_quant_rows_that_hold_no_number(bad, dtype):
+    x = torch.randn(4, 200, generator=torch.Generator().manual_seed(1))
+    x[1, 199] = bad
+    x[3, 0] = bad
+    check_quant(x.to(TYPES[dtype]))
+
+
+# ---- products ------------------------------------------------------------------------------------
+
+def weights(gen, G, N, K, pitch=None):
+    pitch = pitch or (K + 15) // 16 * 16
+    buf = torch.randint(-128, 128, (G, N, pitch), generator=gen, dtype=torch.int8)
+    return buf.cuda()[:, :, :K], (0.5 + torch.rand(G, N, generator=gen)).cuda() / 127
+
+
+def product_tolerance(y, dtype):
+    return np.abs(y) * (3 * U + half_step(dtype)) + 1e-40
+
+
+def swiglu_tolerance(y, want, dtype):
+    """three roundings in front of each factor, which silu multiplies by up to 1 + |g|; exp's error grows with its argument"""
+    g = np.abs(y[:, :y.shape[1] // 2])
+    return np.abs(want) * ((8 * g + 24) * U + half_step(dtype)) + 1e-35
+
+
+def check_product(gen, x, G, N, counts=None, rows=None, row_div=1, swiglu=False, out="bf16", pad_o=0, pitch=None, codes=False, magnitude=None):
+    """x on the host, of its type.  counts: rows of each group (None: one group of all)."""
+    K = x.shape[1]
+    w, ws = weights(gen, G, N, K, pitch)
+    if magnitude:
+        ws *= magnitude
+    offsets = None if counts is None else np.concatenate([[0], np.cumsum(counts)])
+    M = x.shape[0] if rows is None else len(rows)
+    cols = N // 2 if swiglu else N
+    wide = torch.full((M + 2, cols + pad_o), 77.0, dtype=TYPES[out], device="cuda")
+    dev = lambda a: None if a is None else torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")  # noqa: E731
+    q, s = ops.quant_rows(f64(x))
+    kw = dict(offsets=dev(offsets), rows=dev(rows), row_div=row_div, swiglu=swiglu)
+    a = x.cuda()
+    if codes:
+        room = torch.full((x.shape[0], K + (3 if K % 16 else 0)), 55, dtype=torch.int8, device="cuda")    # not zero behind K
+        room[:, :K] = torch.from_numpy(q).cuda()
+        a, kw["a_scale"] = room, torch.from_numpy(s).float().cuda()
+    size = ef.ef_matmul_q8_work(a, w if counts is not None else w[0], ws, wide[:M, :cols], **kw)
+    work = torch.full((size + 64,), 0xA5, dtype=torch.uint8, device="cuda")
+    ef.ef_matmul_q8(a, w if counts is not None else w[0], ws, wide[:M, :cols], work[:size], stream=stream(), **kw)
+    torch.cuda.synchronize()
+    src = None if rows is None else np.asarray(rows) // row_div
+    y = ops.matmul_q8(q, s, w.cpu().numpy(), f64(ws), offsets=offsets, rows=src)
+    inside = M if counts is None else int(offsets[-1])
+    want = y if not swiglu else ops.matmul_q8(q, s, w.cpu().numpy(), f64(ws), offsets=offsets, rows=src, swiglu=True)
+    tol = swiglu_tolerance(y, want, TYPES[out]) if swiglu else product_tolerance(want, TYPES[out])
+    near(wide[:inside, :cols], want[:inside], tol[:inside], f"product M={M} N={N} K={K} G={G} {out} swiglu={swiglu}")
+    assert (wide[inside:] == 77).all() and (wide[:, cols:] == 77).all() and (work[size:] == 0xA5).all()
+
+
+DENSE = [(1, 64, 32), (1, 1, 1), (2, 15, 17), (1, 4096, 48), (16, 64, 64), (17, 80, 33), (33, 1000, 40), (64, 129, 100), (65, 256, 257),
+         (100, 192, 300), (128, 128, 128), (130, 2049, 130), (200, 512, 513), (257, 320, 260), (300, 64, 96), (700, 1000, 520), (1100, 448, 264)]
+
+
+@pytest.mark.parametrize("out", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("M,K,N", DENSE)
+def test_product_of_one_matrix(M, K, N, out):
+    gen = torch.Generator().manual_seed(M + K + N)
+    t = {"bf16": "f32", "f16": "bf16", "f32": "f16"}[out]
+    check_product(gen, torch.randn(M, K, generator=gen).to(TYPES[t]), 1, N, out=out, pad_o=N % 3)
+
+
+@pytest.mark.parametrize("M,K,F", [(1, 64, 16), (1, 2048, 24), (5, 100, 33), (40, 256, 50), (70, 300, 129), (150, 512, 130), (300, 192, 257), (600, 260, 96)])
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+def test_product_with_swiglu(M, K, F, out):
+    gen = torch.Generator().manual_seed(M + K + F)
+    check_product(gen, torch.randn(M, K, generator=gen).bfloat16(), 1, 2 * F, swiglu=True, out=out, magnitude=4 / K ** 0.5, pad_o=1)
+
+
+GROUPS = [
+    # G, counts, K, N
+    (4, [0, 3, 0, 1], 64, 32), (3, [0, 0, 0], 64, 32), (8, [1] * 8, 128, 40), (5, [17, 0, 64, 65, 16], 200, 100), (64, [3] * 60 + [0, 9, 0, 40], 128, 64),
+    (70, [1] * 69 + [5], 64, 16), (300, [i % 4 for i in range(300)], 64, 16), (2, [300, 5], 192, 260), (3, [129, 256, 257], 320, 130),
+    (2, [0, 1000], 256, 512), (6, [600, 1, 31, 0, 255, 97], 448, 256)]
+
+
+@pytest.mark.parametrize("swiglu", [False, True])
+@pytest.mark.parametrize("G,counts,K,N", GROUPS, ids=[f"G{g[0]}-{sum(g[1])}" for g in GROUPS])
+def test_product_of_groups(G, counts, K, N, swiglu):
+    """Product rows of experts, gathered by a permutation of the assignments; rows behind the last group stay as they are."""
+    gen = torch.Generator().manual_seed(G + K)
+    k = 3
+    M = sum(counts) + 4
+    T = (M + k - 1) // k + 1
+    rows = torch.randperm(T * k, generator=gen)[:M].tolist()
+    check_product(gen, torch.randn(T, K, generator=gen).bfloat16(), G, N, counts, rows, k, swiglu, "f32", pad_o=5, magnitude=4 / K ** 0.5)
+
+
+@pytest.mark.parametrize("M,K,N", [(3, 64, 32), (20, 100, 40), (150, 1001, 96), (300, 128, 256), (300, 72, 128)])
+def test_product_of_codes(M, K, N):
+    """Codes and scales from the caller: used in place, or padded first where whole steps cannot be read; what lies behind K is not used."""
+    gen = torch.Generator().manual_seed(M * K)
+    check_product(gen, torch.randn(M, K, generator=gen), 1, N, out="f32", codes=True, pitch=(K + 15) // 16 * 16 + 32)
+
+
+def test_product_of_extreme_codes_is_exact():
+    """All codes -128: sums up to 2^31 - 2^14 at the largest K, exact in 32 bits."""
+    K = 131071
+    a = torch.full((2, K), -128, dtype=torch.int8, device="cuda")
+    w = torch.full((16, 131072), -128, dtype=torch.int8, device="cuda")
+    one = torch.ones(16, device="cuda")
+    out = torch.empty(2, 16, device="cuda")
+    work = torch.empty(ef.ef_matmul_q8_work(a, w[:, :K], one, out, a_scale=one[:2]), dtype=torch.uint8, device="cuda")
+    ef.ef_matmul_q8(a, w[:, :K], one, out, work, a_scale=one[:2], stream=stream())
+    assert (out.double().cpu() == float(np.float32(K * 128 * 128))).all()
+
+
+def test_rows_and_offsets_that_do_not_exist():
+    """Offsets beyond M or descending are clamped, row numbers outside `a` give NaN; nothing is read or written out of range."""
+    gen = torch.Generator().manual_seed(3)
+    x = torch.randn(10, 128, generator=gen).bfloat16()
+    w, ws = weights(gen, 3, 48, 128)
+    q, s = ops.quant_rows(f64(x))
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    for big in (1, 40):       # small groups and large ones: both forms of the kernel
+        M = 10 * big
+        rows = list(range(10)) * big
+        rows[2], rows[5] = -1, 10
+        rows[7] = 2 ** 31 - 1
+        wide = torch.full((M + 3, 48), 5.0, device="cuda")
+        work = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+        ef.ef_matmul_q8(x.cuda(), w, ws, wide[:M], work, rows=i32(rows), offsets=i32([-5, 4 * big, 3 * big, 2 ** 31 - 1]), stream=stream())
+        torch.cuda.synchronize()
+        src = np.array([r if 0 <= r < 10 else 0 for r in rows])
+        y = ops.matmul_q8(q, s, w.cpu().numpy(), f64(ws), offsets=[0, 4 * big, 4 * big, M], rows=src)
+        y[[2, 5, 7]] = np.nan
+        near(wide[:M], y, product_tolerance(y, torch.float32), f"bad rows, M={M}")
+        assert (wide[M:] == 5).all()
+
+
+def test_a_row_without_numbers_gives_a_row_of_nan():
+    gen = torch.Generator().manual_seed(4)
+    x = torch.randn(6, 96, generator=gen)
+    x[2, 50] = float("inf")
+    x[4] = 0
+    check_product(gen, x, 1, 40, out="f32")
+    check_product(gen, x, 1, 40, out="bf16", swiglu=True)
+
+
+# ---- weighted sum --------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("y_type", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("out", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("T,k,d,pad", [(1, 1, 1, 0), (1, 6, 2048, 0), (5, 2, 33, 3), (40, 16, 260, 4), (300, 8, 64, 0), (3, 3, 5000, 8)])
+def test_combine(y_type, out, T, k, d, pad):
+    gen = torch.Generator().manual_seed(T + k + d)
+    y = torch.randn(T * k + 3, d + pad, generator=gen).to(TYPES[y_type]).cuda()
+    w = torch.randn(T, k, generator=gen).cuda()
+    inv = torch.randperm(T * k + 3, generator=gen)[:T * k].int().cuda()
+    for perm in (inv, None):
+        wide = torch.full((T + 1, d + pad), 9.0, dtype=TYPES[out], device="cuda")
+        ef.ef_combine(y[:, :d], w, perm, wide[:T, :d], stream=stream())
+        torch.cuda.synchronize()
+        at = np.arange(T * k) if perm is None else perm.cpu().numpy()
+        want = ops.combine(f64(y[:, :d]), f64(w), at)
+        tol = ops.combine(np.abs(f64(y[:, :d])), np.abs(f64(w)), at) * (k + 1) * U + np.abs(want) * half_step(TYPES[out]) + 2.0 ** -25
+        near(wide[:T, :d], want, tol if out == "f16" else tol - 2.0 ** -25 + 1e-40, f"combine {y_type} {out} {T} {k} {d}")
+        assert (wide[T:] == 9).all() and (wide[:, d:] == 9).all()
+
+
+def test_combine_of_rows_that_do_not_exist():
+    y = torch.ones(4, 8, device="cuda")
+    inv = torch.tensor([0, 1, 4, 2, -1, 3], dtype=torch.int32, device="cuda")
+    out = torch.empty(3, 8, device="cuda")
+    ef.ef_combine(y, torch.ones(3, 2, device="cuda"), inv, out, stream=stream())
+    got = out.cpu()
+    assert (got[0] == 2).all() and got[1:].isnan().all()
+
+
+# ---- together ------------------------------------------------------------------------------------
+
+def layer_inputs(T, E, k, d, F, seed):
+    gen = torch.Generator().manual_seed(seed)
+    x = torch.randn(T, d, generator=gen).bfloat16()
+    z = x.float() @ torch.randn(d, E, generator=gen) / d ** 0.5
+    w13, s13 = weights(gen, E, 2 * F, d)
+    w2, s2 = weights(gen, E, d, F)
+    return x.cuda(), z.cuda(), w13, s13 * 0.5 / d ** 0.5, w2, s2 / F ** 0.5
+
+
+class Layer:
+    def __init__(self, T, E, k, d, F):
+        e = lambda *s, t=torch.int32: torch.empty(*s, dtype=t, device="cuda")  # noqa: E731
+        self.k = k
+        self.ids, self.w, self.counts, self.offsets = e(T, k), e(T, k, t=torch.float32), e(E), e(E + 1)
+        self.perm, self.inv, self.work = e(T * k), e(T * k), e(64 << 20, t=torch.uint8)
+        self.act, self.y, self.out = e(T * k, F, t=torch.bfloat16), e(T * k, d, t=torch.float32), e(T, d, t=torch.bfloat16)
+
+    def __call__(self, x, z, w13, s13, w2, s2, s):
+        ef.ef_route_scores(z, None, self.ids, self.w, self.counts, self.offsets, self.perm, self.inv, self.work, renorm=True, stream=s)
+        ef.ef_matmul_q8(x, w13, s13, self.act, self.work, offsets=self.offsets, rows=self.perm, row_div=self.k, swiglu=True, stream=s)
+        ef.ef_matmul_q8(self.act, w2, s2, self.y, self.work, offsets=self.offsets, stream=s)
+        ef.ef_combine(self.y, self.w, self.inv, self.out, stream=s)
+        return self.out
+
+
+@pytest.mark.parametrize("T,E,k,d,F", [(1, 16, 4, 128, 96), (50, 16, 4, 256, 72), (400, 8, 2, 320, 208)])
+def test_layer_of_the_operators(T, E, k, d, F):
+    """Route, both halves, un-permute: each step against 64 bits on the inputs that it was given."""
+    x, z, w13, s13, w2, s2 = layer_inputs(T, E, k, d, F, T)
+    m = Layer(T, E, k, d, F)
+    out = m(x, z, w13, s13, w2, s2, stream())
+    torch.cuda.synchronize()
+    r = ops.route_scores(f64(z), None, k, renorm=True)
+    assert np.array_equal(m.ids.cpu().numpy(), r["ids"]) and np.array_equal(m.perm.cpu().numpy(), r["perm"])
+    q, s = ops.quant_rows(f64(x))
+    a = dict(offsets=r["offsets"], rows=r["perm"] // k)
+    y = ops.matmul_q8(q, s, w13.cpu().numpy(), f64(s13), **a)
+    act = ops.matmul_q8(q, s, w13.cpu().numpy(), f64(s13), swiglu=True, **a)
+    near(m.act, act, swiglu_tolerance(y, act, torch.bfloat16), "first half")
+    q, s = ops.quant_rows(f64(m.act))
+    y = ops.matmul_q8(q, s, w2.cpu().numpy(), f64(s2), offsets=r["offsets"])
+    near(m.y, y, product_tolerance(y, torch.float32), "second half")
+    want = ops.combine(f64(m.y), f64(m.w), r["inv_perm"])
+    near(out, want, ops.combine(np.abs(f64(m.y)), f64(m.w), r["inv_perm"]) * (k + 1) * U + np.abs(want) * half_step(torch.bfloat16), "un-permute")
+
+
+@pytest.mark.parametrize("T", [3, 400])
+def test_graph_replays_and_other_streams(T):
+    """Captured once, replayed on new inputs between eager calls; eager on a stream of the caller's own.  All give the same bits."""
+    E, k, d, F = 8, 2, 192, 112
+    sets = [layer_inputs(T, E, k, d, F, seed) for seed in (1, 2, 3)]
+    live = [t.clone() for t in sets[0][:2]] + list(sets[0][2:])
+    eager, graphed = Layer(T, E, k, d, F), Layer(T, E, k, d, F)
+    side = torch.cuda.Stream()
+    side.wait_stream(stream())
+    with torch.cuda.stream(side):
+        graphed(*live, stream())
+    stream().wait_stream(side)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        graphed(*live, stream())
+    for x, z, *_ in sets + sets[:1]:
+        want = eager(x, z, *sets[0][2:], stream()).clone()
+        torch.cuda.synchronize()
+        live[0].copy_(x)
+        live[1].copy_(z)
+        graphed.out.fill_(-1)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(graphed.out, want) and torch.equal(graphed.perm, eager.perm)
+        side.wait_stream(stream())
+        with torch.cuda.stream(side):
+            eager(x, z, *sets[0][2:], side)
+        torch.cuda.synchronize()
+        assert torch.equal(eager.out, want)
