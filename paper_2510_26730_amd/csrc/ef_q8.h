@@ -5,8 +5,8 @@
 
 namespace ef {
 
-// a tile of product rows: of one group, rows row0 .. row_end-1 at most `tile` of them
-struct Q8Tile { int group, row0, row_end; };
+// a tile of product rows: rows row0 .. row_end-1 of a group, which has rows lo .. hi-1, `tiles` tiles and the first one's number
+struct Q8Tile { int group, row0, row_end, lo, hi, first, tiles; };
 
 // tiles of `tile` rows that M rows in G groups can make at most: the grid is sized without knowing the groups
 inline int q8_tiles_bound(const Q8Args &p, int tile) {
@@ -14,31 +14,39 @@ inline int q8_tiles_bound(const Q8Args &p, int tile) {
     return p.G == 1 ? (p.M + tile - 1) / tile : full + ragged;
 }
 
-// Tile number `index` of the launch: every wave walks the offsets, 64 groups at a time.  Offsets are clamped to 0..M, and one that
-// lies before an earlier one counts as that one: no tile leaves the M rows and no row is in two groups, whatever they hold.
+// rows of group g, 64 groups from g0 on, one per lane (none past the last group).  Offsets are clamped to 0..M, and one that lies
+// before an earlier one counts as that one (`end`: the largest of the groups before g0), so no tile leaves the M rows and no row is
+// in two groups, whatever they hold.
+__device__ __forceinline__ void q8_group_rows(const Q8Args &p, int g0, int &end, int &lo, int &hi) {
+    const int lane = threadIdx.x & 63, g = g0 + lane;
+    lo = hi = 0;
+    if (g < p.G) {
+        lo = min(max(p.offsets[g], 0), p.M);
+        hi = min(max(p.offsets[g + 1], 0), p.M);
+    }
+    if (__ballot(g < p.G && (lo > hi || lo < end))) {
+        lo = max(lo, end);
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(lo, o);
+            if (lane >= o) lo = max(lo, v);
+        }
+        hi = max(lo, hi);
+    }
+    end = __builtin_amdgcn_readlane(hi, 63);
+}
+
+// Tile number `index` of the launch: every wave walks the offsets
 __device__ __forceinline__ bool q8_find_tile(const Q8Args &p, int index, int tile, Q8Tile &t) {
     if (!p.offsets) {
-        t = Q8Tile{0, index * tile, min(p.M, (index + 1) * tile)};
+        t = Q8Tile{0, index * tile, min(p.M, (index + 1) * tile), 0, p.M, 0, (p.M + tile - 1) / tile};
         return t.row0 < p.M;
     }
     const int lane = threadIdx.x & 63;
-    int before = 0, end = 0;   // tiles and rows of the groups already walked
+    int before = 0, end = 0;
     for (int g0 = 0; g0 < p.G; g0 += 64) {
-        const int g = g0 + lane;
-        int lo = 0, hi = 0;
-        if (g < p.G) {
-            lo = min(max(p.offsets[g], 0), p.M);
-            hi = min(max(p.offsets[g + 1], 0), p.M);
-        }
-        if (__ballot(g < p.G && (lo > hi || lo < end))) {
-            lo = max(lo, end);
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int v = __shfl_up(lo, o);
-                if (lane >= o) lo = max(lo, v);
-            }
-            hi = max(lo, hi);
-        }
+        int lo, hi;
+        q8_group_rows(p, g0, end, lo, hi);
         const int n = (hi - lo + tile - 1) / tile;
         int incl = n;
 #pragma unroll
@@ -49,17 +57,32 @@ __device__ __forceinline__ bool q8_find_tile(const Q8Args &p, int index, int til
         const unsigned long long past = __ballot(before + incl > index);
         if (past) {
             const int l = __builtin_ctzll(past);
-            const int first = before + __builtin_amdgcn_readlane(incl - n, l);
-            const int glo = __builtin_amdgcn_readlane(lo, l), ghi = __builtin_amdgcn_readlane(hi, l);
+            t.first = before + __builtin_amdgcn_readlane(incl - n, l);
+            t.tiles = __builtin_amdgcn_readlane(n, l);
+            t.lo = __builtin_amdgcn_readlane(lo, l);
+            t.hi = __builtin_amdgcn_readlane(hi, l);
             t.group = g0 + l;
-            t.row0 = glo + (index - first) * tile;
-            t.row_end = min(ghi, t.row0 + tile);
+            t.row0 = t.lo + (index - t.first) * tile;
+            t.row_end = min(t.hi, t.row0 + tile);
             return true;
         }
         before += __builtin_amdgcn_readlane(incl, 63);
-        end = __builtin_amdgcn_readlane(hi, 63);
     }
     return false;
+}
+
+// tiles of `tile` rows that the groups make
+__device__ __forceinline__ int q8_total_tiles(const Q8Args &p, int tile) {
+    if (!p.offsets) return (p.M + tile - 1) / tile;
+    int total = 0, end = 0;
+    for (int g0 = 0; g0 < p.G; g0 += 64) {
+        int lo, hi;
+        q8_group_rows(p, g0, end, lo, hi);
+        int n = (hi - lo + tile - 1) / tile;
+        for (int o = 32; o >= 1; o >>= 1) n += __shfl_xor(n, o);
+        total += __builtin_amdgcn_readfirstlane(n);
+    }
+    return total;
 }
 
 // the row of `a` behind a product row, and its scale; one that does not exist reads row 0 and counts as NaN
@@ -79,6 +102,18 @@ __device__ __forceinline__ void store_element(void *out, size_t at, float v) {
     if constexpr (TYPE == EF_F32) static_cast<float *>(out)[at] = v;
     else if constexpr (TYPE == EF_F16) static_cast<_Float16 *>(out)[at] = (_Float16)v;
     else static_cast<__bf16 *>(out)[at] = (__bf16)v;
+}
+
+// four results, as the output type, into columns c .. c+3 of a row in LDS
+__device__ __forceinline__ void q8_put4(char *row, int c, int type, const float (&v)[4]) {
+    if (type == EF_F32) *reinterpret_cast<float4 *>(row + c * 4) = make_float4(v[0], v[1], v[2], v[3]);
+    else if (type == EF_F16) {
+        typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<h4 *>(row + c * 2) = h4{(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
+    } else {
+        typedef __bf16 b4 __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<b4 *>(row + c * 2) = b4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+    }
 }
 
 // columns n .. n+3 of an output row, as far as they are below n_end

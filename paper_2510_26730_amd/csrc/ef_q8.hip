@@ -236,6 +236,7 @@ hipError_t launch_quant_rows(const QuantArgs &a, hipStream_t s) {
 hipError_t launch_q8_product(const Q8Args &p, hipStream_t s) {
     if (p.M <= 0) return hipSuccess;
     const int per = (p.M + p.G - 1) / p.G;
+    if (per > 64) return launch_q8_tiled(p, per > 512, s);
     if (p.swiglu) return per <= 16 ? launch_stream<1, true>(p, s) : per <= 32 ? launch_stream<2, true>(p, s) : launch_stream<4, true>(p, s);
     return per <= 16 ? launch_stream<1, false>(p, s) : per <= 32 ? launch_stream<2, false>(p, s) : launch_stream<4, false>(p, s);
 }

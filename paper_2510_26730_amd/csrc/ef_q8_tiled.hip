@@ -1,0 +1,221 @@
+// Products of 8-bit codes, tiled: many rows per matrix, bound by the matrix cores.
+//
+// A workgroup of four waves owns 64*RA matrix rows (output columns) x 64*RB product rows, a wave a quarter of it: RA x RB
+// accumulators of v_mfma_i32_32x32x32_i8, 32-bit whole numbers.  Both operands come row by row as the caller has them, so the rows
+// of `a` are gathered by the routing for free: direct global -> LDS loads of 16 rows x 64 bytes (a wave's 64 lanes x 16 bytes, a
+// "slab") fill a ring of four stages of 64 codes of K, three ahead of the one that feeds the matrix cores, one barrier per stage.
+// Rows of 64 bytes would put every second row of an operand read into the same LDS banks, so lane 4r + p of a load fetches chunk
+// p ^ fold(r) of its row instead of p: the 16-byte chunks of a slab lie permuted within their row, and a read of 32 rows at one
+// chunk touches all banks evenly.
+// The results go through LDS on their way out, so that a wave stores whole runs of a row.
+#include "ef_device.h"
+#include "ef_kernels.h"
+#include "ef_ops.h"
+#include "ef_q8.h"
+
+namespace ef {
+
+namespace {
+
+typedef int int4v __attribute__((ext_vector_type(4)));
+typedef int int16v __attribute__((ext_vector_type(16)));
+
+constexpr int kStages = 4;
+constexpr int wait_vm(int n) { return ((n >> 4) << 14) | (0x7 << 4) | (0xF << 8) | (n & 15); }   // s_waitcnt vmcnt(n) alone
+__device__ __forceinline__ int fold(int r) { return (r >> 1 ^ r >> 3) & 3; }
+
+// 64 lanes x 16 bytes straight into LDS at a wave-uniform byte offset; in inline assembly so that the compiler neither moves it
+// against the LDS reads nor waits for it: every wait for these loads is an explicit vmcnt
+#define EF_Q8_DMA(gptr, lds_off) \
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(gptr), "s"(lds_off) : "memory")
+
+// After matrix product m of a K step: which operand reads (of 8 / 4, in the order a0 b0 a1 b1 ..) and which loads go out there.
+// 16 products: reads in the first ten slots, so the next step never waits; loads evenly, because a burst stalls at the issue.
+template <int RA, int RB> struct Slots;
+template <> struct Slots<4, 4> {
+    static constexpr int read(int m) { constexpr int r[16] = {0, 1, -1, 2, 3, 4, -1, 5, 6, 7, -1, -1, -1, -1, -1, -1}; return r[m]; }
+    static constexpr int load(int m) { return m % 4 == 2 ? m / 4 : -1; }
+};
+template <> struct Slots<2, 2> {
+    static constexpr int read(int m) { return m; }
+    static constexpr int load(int m) { return m % 2 == 0 ? m / 2 : -1; }
+};
+
+template <int I, int N, class F>
+__device__ __forceinline__ void static_for(F &&f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        static_for<I + 1, N>(f);
+    }
+}
+
+template <int RA, int RB, bool PAIR>
+__global__ __launch_bounds__(256, RA *RB >= 16 ? 1 : 2) void q8_tiled_kernel(Q8Args p, int npanels) {
+    static_assert(RA == RB, "reads alternate between the operands");
+    constexpr int kSlabs = 4 * (RA + RB), kStageBytes = kSlabs * 1024, kLoads = RA + RB;
+    __shared__ __attribute__((aligned(16))) char lds[kStages * kStageBytes];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wf = wave & 1, wt = wave >> 1;
+
+    // the unit of this workgroup: an even, contiguous share of all units per XCD (workgroups go to the XCDs in turn)
+    const int units = q8_total_tiles(p, 64 * RB) * npanels, part = blockIdx.x & 7;
+    const int u = tiled_xcd_begin(units, part) + (int)(blockIdx.x >> 3);
+    if (u >= tiled_xcd_begin(units, part + 1)) return;
+    Q8Tile t;
+    if (!q8_find_tile(p, u / npanels, 64 * RB, t)) return;
+    const TiledUnit unit = tiled_unit(u - t.first * npanels, npanels, t.tiles);
+    t.row0 = t.lo + unit.mp * 64 * RB;
+    t.row_end = min(t.hi, t.row0 + 64 * RB);
+    const int F = p.N >> 1, n_end = PAIR ? F : p.N;
+    const int n0 = unit.np * (PAIR ? 32 * RA : 64 * RA);
+    const int nstage = (p.K + 63) >> 6;
+
+    // this lane's rows; columns past the end and rows past the group's read a neighbour's codes, their results are dropped
+    const int8_t *wsrc[RA], *xsrc[RB];
+#pragma unroll
+    for (int q = 0; q < RA; ++q) {
+        const int local = (q * 4 + wave) * 16 + (lane >> 2), i = local & 31, ab = local >> 5;
+        const int row = PAIR ? (ab & 1) * F + min(n0 + (ab >> 1) * 32 + i, F - 1) : min(n0 + local, p.N - 1);
+        wsrc[q] = p.w + (size_t)t.group * p.w_group + (size_t)row * p.ldw;
+    }
+#pragma unroll
+    for (int q = 0; q < RB; ++q) {
+        const int local = (q * 4 + wave) * 16 + (lane >> 2);
+        xsrc[q] = p.a + (size_t)q8_row(p, min(t.row0 + local, t.row_end - 1)).row * p.lda;
+    }
+    const int chunk = ((lane & 3) ^ fold(lane >> 2)) * 16;
+    const int k_last = ((p.K + 15) & ~15) - 16;   // last 16 codes that a weight row holds; beyond K the rows of `a` are zero
+    const unsigned lds_base = (unsigned)(size_t)&lds[0];
+    // load `q` of stage `st` (past the end the last stage again, in bounds): waits count loads, so every wave issues all of them
+    const auto load = [&](int st, auto q) {
+        constexpr int n = decltype(q)::value;
+        const int k = min(st, nstage - 1) * 64 + chunk;
+        const int8_t *from = n < RA ? wsrc[n < RA ? n : 0] + min(k, k_last) : xsrc[n < RA ? 0 : n - RA] + k;
+        const unsigned to = lds_base + (st & (kStages - 1)) * kStageBytes + (n < RA ? n * 4 : 4 * RA + (n - RA) * 4) * 1024 + wave * 1024;
+        EF_Q8_DMA(from, to);
+    };
+    // operand fragment `blk` of 32 rows, K step ks of a stage: row i of the fragment, 16 bytes at 32 ks + 16 (lane / 32)
+    const int i = lane & 31, row_at = (i >> 4) * 1024 + (i & 15) * 64;
+    const int at0 = row_at + (((lane >> 5) ^ fold(i & 15)) << 4), at1 = at0 ^ 32;
+    const int abase = wf * RA * 2048, bbase = (4 * RA + wt * RB * 2) * 1024;
+    const auto frag = [&](int st, int ks, int base, int blk) {
+        return *reinterpret_cast<const int4v *>(lds + (st & (kStages - 1)) * kStageBytes + base + blk * 2048 + (ks ? at1 : at0));
+    };
+
+    int16v acc[RA][RB];
+#pragma unroll
+    for (int x = 0; x < RA; ++x)
+#pragma unroll
+        for (int y = 0; y < RB; ++y)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[x][y][v] = 0;
+    int4v a0[RA], b0[RB], a1[RA], b1[RB];
+
+    static_for<0, kStages - 1>([&](auto st) { static_for<0, kLoads>([&](auto q) { load(decltype(st)::value, q); }); });
+    __builtin_amdgcn_s_waitcnt(wait_vm(kLoads * (kStages - 2)));   // my part of stage 0 has landed
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < RA; ++x) a0[x] = frag(0, 0, abase, x);
+#pragma unroll
+    for (int y = 0; y < RB; ++y) b0[y] = frag(0, 0, bbase, y);
+
+    // one K step: the products of (ac, bc), the reads of the next step's (an, bn), half of the loads of stage `ld`.  Only the
+    // first `LIVE` of the wave's row tiles exist; the products of the others are left out (power is what limits a full chip).
+    const auto step = [&](auto LIVE, int4v(&ac)[RA], int4v(&bc)[RB], int4v(&an)[RA], int4v(&bn)[RB], int rd, int rks, int ld, auto half) {
+        constexpr int live = decltype(LIVE)::value;
+        static_for<0, RA * RB>([&](auto M) {
+            constexpr int m = decltype(M)::value, x = m / RB, y = m % RB, r = Slots<RA, RB>::read(m), l = Slots<RA, RB>::load(m);
+            if constexpr (y < live) acc[x][y] = __builtin_amdgcn_mfma_i32_32x32x32_i8(ac[x], bc[y], acc[x][y], 0, 0, 0);
+            if constexpr (r >= 0 && r % 2 == 0) an[r / 2] = frag(rd, rks, abase, r / 2);
+            if constexpr (r >= 0 && r % 2 == 1 && r / 2 < live) bn[r / 2] = frag(rd, rks, bbase, r / 2);
+            if constexpr (l >= 0) load(ld, std::integral_constant<int, decltype(half)::value * (kLoads / 2) + l>{});
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    const auto loop = [&](auto LIVE) {
+        for (int st = 0; st < nstage; ++st) {
+            // the buffer of stage st+3 held stage st-1, whose last reads every wave finished before the previous barrier
+            step(LIVE, a0, b0, a1, b1, st, 1, st + kStages - 1, std::integral_constant<int, 0>{});
+            __builtin_amdgcn_s_waitcnt(wait_vm(kLoads * (kStages - 3) + kLoads / 2));   // stage st+1 has landed
+            __syncthreads();
+            __builtin_amdgcn_sched_barrier(0);
+            step(LIVE, a1, b1, a0, b0, st + 1, 0, st + kStages - 1, std::integral_constant<int, 1>{});
+        }
+    };
+    const int live = max(0, min(RB, (t.row_end - t.row0 - wt * 32 * RB + 31) / 32));
+    if (live == RB) loop(std::integral_constant<int, RB>{});
+    else if (RB > 3 && live == 3) loop(std::integral_constant<int, (RB > 3 ? 3 : 1)>{});
+    else if (RB > 2 && live == 2) loop(std::integral_constant<int, (RB > 2 ? 2 : 1)>{});
+    else if (live == 1) loop(std::integral_constant<int, 1>{});
+    else loop(std::integral_constant<int, 0>{});
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+
+    // Lane 32g + i holds product row i of its tile, columns 8q + 4g .. +3 of each fragment.  Tile by tile through this wave's
+    // share of the ring: 16 bytes per lane back, neighbouring lanes neighbouring pieces of a row.
+    constexpr int kCols = PAIR ? 16 * RA : 32 * RA;        // output columns of the wave
+    const int g = lane >> 5, col0 = n0 + wf * kCols;
+    const float *ws = p.w_scale + (size_t)t.group * p.N;
+    float sc[RA][16];
+#pragma unroll
+    for (int x = 0; x < RA; ++x)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int c = 8 * (v >> 2) + 4 * g + (v & 3);
+            sc[x][v] = PAIR ? ws[(x & 1) * F + min(col0 + (x >> 1) * 32 + c, F - 1)] : ws[min(col0 + x * 32 + c, p.N - 1)];
+        }
+    const int size = p.out_type == EF_F32 ? 4 : 2, pitch = kCols * size + 16;
+    char *mine = lds + wave * (kStages * kStageBytes / 4);
+    static_assert(32 * (kCols * 4 + 16) <= kStages * kStageBytes / 4, "a tile of results fits a wave's share of the ring");
+    const bool whole = ((reinterpret_cast<size_t>(p.out) | (size_t)p.ldo * size) & 15) == 0 && (col0 * size & 15) == 0;
+#pragma unroll
+    for (int y = 0; y < RB; ++y) {
+        const int row0 = t.row0 + (wt * RB + y) * 32;
+        if (row0 >= t.row_end) break;
+        const float xs = q8_row(p, min(row0 + i, t.row_end - 1)).scale;
+#pragma unroll
+        for (int x = 0; x < RA; x += PAIR ? 2 : 1)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = (float)acc[x][y][4 * q + e] * xs * sc[x][4 * q + e];
+                    if constexpr (PAIR) v[e] = silu_mul(v[e], (float)acc[x + 1][y][4 * q + e] * xs * sc[x + 1][4 * q + e]);
+                }
+                q8_put4(mine + i * pitch, (PAIR ? x / 2 : x) * 32 + 8 * q + 4 * g, p.out_type, v);
+            }
+        wave_lds_sync();
+        const int per_row = kCols * size / 16, rows = min(32, t.row_end - row0);
+        for (int z = lane; z < 32 * per_row; z += 64) {
+            const int r = z / per_row, piece = z - r * per_row, elems = 16 / size, c = col0 + piece * elems;
+            if (r >= rows || c >= n_end) continue;
+            const char *from = mine + r * pitch + piece * 16;
+            char *to = static_cast<char *>(p.out) + ((size_t)(row0 + r) * p.ldo + c) * size;
+            if (whole && c + elems <= n_end) *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(from);
+            else if (size == 4)
+                for (int e = 0; e < 4 && c + e < n_end; ++e) reinterpret_cast<float *>(to)[e] = reinterpret_cast<const float *>(from)[e];
+            else
+                for (int e = 0; e < 8 && c + e < n_end; ++e) reinterpret_cast<uint16_t *>(to)[e] = reinterpret_cast<const uint16_t *>(from)[e];
+        }
+        wave_lds_sync();
+    }
+}
+
+template <int R, bool PAIR>
+hipError_t launch(const Q8Args &p, hipStream_t s) {
+    const int cols = PAIR ? p.N / 2 : p.N, per = PAIR ? 32 * R : 64 * R, npanels = (cols + per - 1) / per;
+    const long long units = (long long)q8_tiles_bound(p, 64 * R) * npanels;
+    if (units > 0x7FFFFFF0ll) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((q8_tiled_kernel<R, R, PAIR>), dim3((unsigned)((units + 7) / 8 * 8)), dim3(256), 0, s, p, npanels);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_q8_tiled(const Q8Args &p, bool wide, hipStream_t s) {
+    if (p.swiglu) return wide ? launch<4, true>(p, s) : launch<2, true>(p, s);
+    return wide ? launch<4, false>(p, s) : launch<2, false>(p, s);
+}
+
+}  // namespace ef
