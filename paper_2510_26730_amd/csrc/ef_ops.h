@@ -9,7 +9,7 @@
 namespace ef {
 
 // ---- routing from logits (ef_router.hip) -------------------------------------------------------
-constexpr int kRouterWaves = 16;        // waves of a workgroup; one token per wave at a time
+constexpr int kRouterSumTiles = 1024;   // tiles whose counts every workgroup of the scatter adds up by itself
 
 struct RouterArgs {
     ef_router r;
@@ -22,7 +22,9 @@ struct RouterArgs {
     float *w;
     int32_t *counts, *offsets, *perm, *inv_perm;
     int ntiles;            // token tiles of router_tile(T) tokens
-    int32_t *tile_counts;  // [E][ntiles] (scratch): assignments of a tile to an expert, then their prefixes over the tiles
+    uint8_t *tile_counts;  // [ntiles][pitch] (scratch): assignments of a tile to an expert
+    int pitch;             // E rounded up to 16
+    int32_t *prefix;       // [ntiles][pitch] (scratch): their prefixes over the tiles; null for up to kRouterSumTiles tiles
     uint8_t *rank;         // [T*k] (scratch): earlier tokens of the tile with the same expert
 };
 int router_tile(int T);

@@ -33,13 +33,15 @@ const char *router_fault(const ef_router *r) {
 bool router_tokens_ok(const ef_router *r, int T) { return T >= 0 && (long long)T * r->top_k <= 0x7FFFFFFFll; }
 
 int router_tiles(int T) { return (T + ef::router_tile(T) - 1) / ef::router_tile(T); }
-size_t router_counts_bytes(const ef_router *r, int T) { return rounded((size_t)4 * r->n_experts * router_tiles(T)); }
+int router_pitch(const ef_router *r) { return (r->n_experts + 15) / 16 * 16; }
+size_t router_counts_bytes(const ef_router *r, int T) { return rounded((size_t)router_pitch(r) * router_tiles(T)); }
+size_t router_prefix_bytes(const ef_router *r, int T) { return router_tiles(T) > ef::kRouterSumTiles ? 4 * router_counts_bytes(r, T) : 0; }
 
 }  // namespace
 
 extern "C" size_t ef_route_scores_work(const ef_router *r, int T) {
     if (router_fault(r) || !router_tokens_ok(r, T)) return 0;
-    return router_counts_bytes(r, T) + rounded((size_t)T * r->top_k) + kAlign;
+    return router_counts_bytes(r, T) + router_prefix_bytes(r, T) + rounded((size_t)T * r->top_k) + kAlign;
 }
 
 extern "C" int ef_route_scores(const ef_router *r, const void *logits, int type, int64_t ld, const float *bias, int T,
@@ -72,8 +74,10 @@ extern "C" int ef_route_scores(const ef_router *r, const void *logits, int type,
     a.perm = perm;
     a.inv_perm = inv_perm;
     a.ntiles = router_tiles(T);
-    a.tile_counts = static_cast<int32_t *>(work);
-    a.rank = static_cast<uint8_t *>(work) + router_counts_bytes(r, T);
+    a.tile_counts = static_cast<uint8_t *>(work);
+    a.pitch = router_pitch(r);
+    a.prefix = router_prefix_bytes(r, T) ? reinterpret_cast<int32_t *>(a.tile_counts + router_counts_bytes(r, T)) : nullptr;
+    a.rank = a.tile_counts + router_counts_bytes(r, T) + router_prefix_bytes(r, T);
     EF_HIP(nullptr, ef::launch_router(a, static_cast<hipStream_t>(stream)));
     return EF_OK;
 }

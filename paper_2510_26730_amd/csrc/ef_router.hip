@@ -1,18 +1,26 @@
 // Routing from logits: scores, balance bias, groups of experts, top-k, weights, and the stable grouping of the assignments.
 //
-// A wave takes one token: expert e sits in lane e % 64, register e / 64.  The choice values c become whole numbers of the same
-// order ("keys": a float's bits, negative ones inverted), so a maximum over the wave is six DPP steps on 32-bit numbers.  Top-k
-// is k such maxima; the lowest expert with the maximum's key is found by ballots, so ties need no second key.
-// Without a bias (and without sums of two) the order of the logits is the order of the scores, and the logits themselves are
-// compared, exactly.  Otherwise c is formed in 32 bits, where it is off by up to ~1e-6 of the largest score and of the bias; a
-// token whose border (the last chosen against the best left out, of experts or of groups) is closer than that is decided again in
-// 64 bits: with 256 experts one token in some thousands, where forming every score in 64 bits would cost more than the logits' bytes.
+// A wave takes four tokens, 16 lanes each; lane l of a token holds the experts l*V .. l*V+V-1, V = ceil(E / 16).  A choice value
+// becomes a whole number of the same order (a float's bits, negative ones inverted) whose low nine bits are replaced by 511 - e:
+// keys are distinct, a maximum names its expert and ties go to the lowest.  Top-k is k rounds of "the largest key below the last
+// one": key - last, modulo 2^32, is largest for exactly that key, so nothing has to be removed between rounds, and a round is 1.5
+// instructions per key and four DPP steps for four tokens.
+// The nine bits, and forming scores in 32 bits (not needed without a bias, where the order of the logits is that of the scores, and
+// exact where logits have 16 bits), can hide which of two close values is larger.  That matters at a border only: the last expert
+// chosen against the best left out, the last group kept against the best dropped.  A token whose border is closer than the error is
+// decided again by the whole wave, from its logits' full bits or from scores in 64 bits ("exact" below): with 256 experts some
+// tokens in a thousand.  Groups that 16 lanes cannot share evenly go that way always.
+//
+// Bound by instructions: 32768 tokens of 256 experts need ~200 per token, MEASURED_HERE.
 //
 // Grouping: a workgroup takes one tile of 16 or 64 tokens, and every expert has a bit per token of the tile in LDS.  The bits
 // below a token's own are its rank among the tile's assignments to that expert, their number the tile's count.  One tile:
-// everything in one launch.  Otherwise the counts' prefixes over the tiles, a wave per expert, and a scatter, a tile per workgroup.
+// everything in one launch.  Otherwise a second launch adds up the tiles' counts, all of them and those before its own tile, in
+// every workgroup, and scatters.
 #include "ef_device.h"
 #include "ef_ops.h"
+
+#include <type_traits>
 
 namespace ef {
 
@@ -21,9 +29,9 @@ hipError_t launch_fill_i32(int32_t *p, int n, int32_t v, hipStream_t s);
 namespace {
 
 // DPP moves within a wave; lanes without a source get 0
-template <int CTRL, int ROWS = 0xf>
+template <int CTRL>
 __device__ __forceinline__ uint32_t dpp0(uint32_t x) {
-    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, false);
 }
 constexpr int kShr1 = 0x111, kShr2 = 0x112, kShr4 = 0x114, kShr8 = 0x118, kBcast15 = 0x142, kBcast31 = 0x143;
 
@@ -42,16 +50,6 @@ __device__ __forceinline__ uint64_t wave_max(uint64_t x) {
     return (uint64_t)hi << 32 | lo;
 }
 // sum over the wave in a fixed order
-__device__ __forceinline__ float wave_sum(float x) {
-    const auto add = [](float v, uint32_t o) { return v + __builtin_bit_cast(float, o); };
-    x = add(x, dpp0<kShr1>(__builtin_bit_cast(uint32_t, x)));
-    x = add(x, dpp0<kShr2>(__builtin_bit_cast(uint32_t, x)));
-    x = add(x, dpp0<kShr4>(__builtin_bit_cast(uint32_t, x)));
-    x = add(x, dpp0<kShr8>(__builtin_bit_cast(uint32_t, x)));
-    x = add(x, dpp0<kBcast15, 0xa>(__builtin_bit_cast(uint32_t, x)));
-    x = add(x, dpp0<kBcast31, 0xc>(__builtin_bit_cast(uint32_t, x)));
-    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
-}
 __device__ __forceinline__ double wave_sum(double x) {
     for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off);
     return x;
@@ -76,17 +74,40 @@ __device__ __forceinline__ uint64_t key_of(double f) {
     const uint64_t u = __builtin_bit_cast(uint64_t, f);
     return u >> 63 ? ~u : u | 0x8000000000000000ull;
 }
-__device__ __forceinline__ double of_key(uint64_t k) {
-    return __builtin_bit_cast(double, k >> 63 ? k & 0x7FFFFFFFFFFFFFFFull : ~k);
-}
 
+template <int TYPE, class T>
+__device__ __forceinline__ float value_of(T b) {
+    if constexpr (TYPE == EF_F32) return b;
+    else if constexpr (TYPE == EF_BF16) return __builtin_bit_cast(float, (uint32_t)b << 16);
+    else return (float)__builtin_bit_cast(_Float16, b);
+}
 __device__ __forceinline__ float load_element(const void *p, int type, size_t i) {
     if (type == EF_F32) return static_cast<const float *>(p)[i];
     const uint16_t b = static_cast<const uint16_t *>(p)[i];
-    return type == EF_BF16 ? __builtin_bit_cast(float, (uint32_t)b << 16) : (float)__builtin_bit_cast(_Float16, b);
+    return type == EF_BF16 ? value_of<EF_BF16>(b) : value_of<EF_F16>(b);
 }
 
 constexpr float kMinusInf = -__builtin_inff();
+// NaN counts as -inf, -0 and 0 are one value
+__device__ __forceinline__ float clean(float x) { return x != x ? kMinusInf : x + 0.f; }
+
+// maximum of numbers that are not NaN, without the canonicalising that fmaxf brings
+__device__ __forceinline__ float max_of(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, __builtin_inff()); }
+__device__ __forceinline__ float min_of(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, -__builtin_inff()); }
+
+// keeps a value out of a branch that the compiler would make of a selection behind it
+__device__ __forceinline__ float pinned(float x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+template <int I, int N, class F>
+__device__ __forceinline__ void static_for(F &&f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        static_for<I + 1, N>(f);
+    }
+}
 
 struct Groups {
     int n, size, kept, best;
@@ -94,12 +115,11 @@ struct Groups {
 };
 
 // Chooses a token's experts by their choice values c (expert r*64 + lane; `mine`: bits of the registers that hold an expert).
-// Returns the bits of the lane's chosen registers; `near`: a border is closer than `margin`.  cl: this wave's LDS, for the groups.
+// Returns the bits of the lane's chosen registers.  cl: this wave's LDS, for the groups.
 template <int R, class V>
-__device__ __forceinline__ uint32_t choose(const V (&c)[R], uint32_t mine, int k, const Groups &g, V *cl, V margin, bool &near) {
+__device__ __forceinline__ uint32_t choose(const V (&c)[R], uint32_t mine, int k, const Groups &g, V *cl) {
     const int lane = threadIdx.x & 63;
     uint32_t live = mine;
-    near = false;
     if (g.n > 1) {
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -125,12 +145,7 @@ __device__ __forceinline__ uint32_t choose(const V (&c)[R], uint32_t mine, int k
             const V ov = lane_value(v, o * g.lanes);
             rank += ov > v || (ov == v && o < grp);
         }
-        const bool leads = q == 0 && grp < g.n;
-        const unsigned long long kept = __ballot(leads && rank < g.kept);
-        if (g.kept < g.n) {
-            const unsigned long long last = __ballot(leads && rank == g.kept - 1), next = __ballot(leads && rank == g.kept);
-            near = lane_value(v, __builtin_ctzll(last)) - lane_value(v, __builtin_ctzll(next)) <= margin;
-        }
+        const unsigned long long kept = __ballot(q == 0 && grp < g.n && rank < g.kept);
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (mine >> r & 1 && !(kept >> ((r * 64 + lane) / g.size * g.lanes) & 1)) live &= ~(1u << r);
@@ -140,29 +155,21 @@ __device__ __forceinline__ uint32_t choose(const V (&c)[R], uint32_t mine, int k
 #pragma unroll
     for (int r = 0; r < R; ++r) key[r] = live >> r & 1 ? key_of(c[r]) : 0;
     uint32_t chosen = 0;
-    Key last = 0;
     for (int j = 0; j < k; ++j) {
         Key m = key[0];
 #pragma unroll
         for (int r = 1; r < R; ++r) m = max(m, key[r]);
-        last = wave_max(m);
+        m = wave_max(m);
         bool found = false;   // uniform
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const unsigned long long eq = __ballot(!found && key[r] == last);
+            const unsigned long long eq = __ballot(!found && key[r] == m);
             if (eq && lane == __builtin_ctzll(eq)) {
                 chosen |= 1u << r;
                 key[r] = 0;
             }
             found |= eq != 0;
         }
-    }
-    if (margin >= 0) {   // uniform
-        Key m = key[0];
-#pragma unroll
-        for (int r = 1; r < R; ++r) m = max(m, key[r]);
-        const Key next = wave_max(m);
-        near |= next != 0 && of_key(last) - of_key(next) <= margin;
     }
     return chosen;
 }
@@ -186,142 +193,375 @@ __device__ __forceinline__ int expert_offsets(const int (&cnt)[R], int (&off)[R]
     return before;
 }
 
-template <int TT> struct TileBits { using type = unsigned long long; };
-template <> struct TileBits<16> { using type = uint32_t; };
+// ---- the exact way: a whole wave decides one token; expert r*64 + lane in register r -----------------------------------------
 
-template <int R, int TT>
-__global__ __launch_bounds__(64 * kRouterWaves) void router_kernel(RouterArgs a) {
-    using Bits = typename TileBits<TT>::type;
-    constexpr int kE = 64 * R;
-    __shared__ Bits bits[kE];
-    __shared__ uint16_t chosen_ids[TT * EF_ROUTER_MAX_TOPK];
-    __shared__ int first[kE];
-    __shared__ double group_values[kRouterWaves][kE];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int E = a.r.n_experts, k = a.r.top_k;
-    const int t0 = blockIdx.x * TT, n = min(TT, a.T - t0);
-    for (int e = tid; e < kE; e += 64 * kRouterWaves) bits[e] = 0;
-    __syncthreads();
-
-    Groups g{a.r.n_groups, E / a.r.n_groups, a.r.groups_kept, a.r.group_best, 64};
-    while (g.lanes * g.n > 64) g.lanes >>= 1;
+// ids and weights of token t (in the batch; `bit` its number in the tile)
+template <int R, class Bits>
+__device__ __forceinline__ void exact_token(const RouterArgs &a, size_t t, int bit, const Groups &g, double *cl, uint16_t *chosen_ids, Bits *bits) {
+    const int lane = threadIdx.x & 63, E = a.r.n_experts, k = a.r.top_k;
     const bool softmax = a.r.score == EF_SCORE_SOFTMAX;
-    const bool by_logit = !a.bias && (g.n == 1 || g.best == 1);
+    float z[R];
     uint32_t mine = 0;
-    float b[R], bmax = 0.f;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int e = r * 64 + lane;
-        b[r] = 0.f;
+        z[r] = kMinusInf;
         if (e < E) {
             mine |= 1u << r;
-            if (a.bias) {
-                b[r] = a.bias[e];
-                if (b[r] != b[r]) b[r] = kMinusInf;
-                if (fabsf(b[r]) < __builtin_inff()) bmax = fmaxf(bmax, fabsf(b[r]));
-            }
+            z[r] = clean(load_element(a.logits, a.type, t * a.ld + e));
         }
     }
-    if (a.bias) bmax = __builtin_bit_cast(float, wave_max(__builtin_bit_cast(uint32_t, bmax)));
-
-    float zn[R];   // the next token's logits
-    const auto fetch = [&](int t) {
+    uint32_t mk = 0;
 #pragma unroll
-        for (int r = 0; r < R; ++r)
-            zn[r] = mine >> r & 1 ? load_element(a.logits, a.type, (size_t)(t0 + t) * a.ld + r * 64 + lane) : kMinusInf;
+    for (int r = 0; r < R; ++r) mk = max(mk, key_of(z[r]));
+    const float m = of_key(wave_max(mk));
+    uint32_t chosen;
+    double total = 0;      // softmax: sum of exp(z - m)
+    if (softmax) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) total += z[r] == kMinusInf ? 0 : z[r] == m ? 1 : exp((double)z[r] - (double)m);
+        total = wave_sum(total);
+    }
+    const auto score = [&](float x) -> double {
+        if (!softmax) return 1 / (1 + exp(-(double)x));
+        return x == kMinusInf ? 0 : (x == m ? 1 : exp((double)x - (double)m)) / total;   // m = inf: the others are 0
     };
-    if (wave < n) fetch(wave);
-    for (int t = wave; t < n; t += kRouterWaves) {
-        float z[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) z[r] = zn[r] != zn[r] ? kMinusInf : zn[r] + 0.f;   // -0 and 0 are one value
-        if (t + kRouterWaves < n) fetch(t + kRouterWaves);
-
-        // scores in 32 bits
-        float s[R], top = 1.f;
-        if (softmax) {
-            uint32_t mk = 0;
-#pragma unroll
-            for (int r = 0; r < R; ++r) mk = max(mk, key_of(z[r]));
-            const float m = of_key(wave_max(mk));
-            float part = 0.f;
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                s[r] = z[r] == kMinusInf ? 0.f : z[r] == m ? 1.f : expf(z[r] - m);   // m = inf: the others are 0
-                part += s[r];
-            }
-            const float sum = wave_sum(part);
-            const float inv = sum > 0.f ? 1.f / sum : 0.f;
-#pragma unroll
-            for (int r = 0; r < R; ++r) s[r] *= inv;
-            top = inv;
-        } else {
-#pragma unroll
-            for (int r = 0; r < R; ++r) s[r] = 1.f / (1.f + expf(-z[r]));
-        }
-
-        uint32_t chosen;
-        bool near;
-        if (by_logit) {
-            chosen = choose<R, float>(z, mine, k, g, reinterpret_cast<float *>(group_values[wave]), -1.f, near);
-        } else {
-            float c[R];
-#pragma unroll
-            for (int r = 0; r < R; ++r) c[r] = z[r] == kMinusInf ? kMinusInf : s[r] + b[r];
-            // a choice value is off by at most 1.2e-6 of the largest score and 2^-24 of itself, a sum of two by twice that
-            chosen = choose<R, float>(c, mine, k, g, reinterpret_cast<float *>(group_values[wave]), 8e-6f * top + 1e-6f * bmax, near);
-            if (near) {
-                double d[R];
-                if (softmax) {
-                    float m = kMinusInf;
-#pragma unroll
-                    for (int r = 0; r < R; ++r) m = fmaxf(m, z[r]);
-                    m = of_key(wave_max(key_of(m)));
-                    double part = 0;
-#pragma unroll
-                    for (int r = 0; r < R; ++r) {
-                        d[r] = z[r] == kMinusInf ? 0 : z[r] == m ? 1 : exp((double)z[r] - (double)m);
-                        part += d[r];
-                    }
-                    const double sum = wave_sum(part);
-#pragma unroll
-                    for (int r = 0; r < R; ++r) d[r] = sum > 0 ? d[r] / sum : 0;
-                } else {
-#pragma unroll
-                    for (int r = 0; r < R; ++r) d[r] = 1 / (1 + exp(-(double)z[r]));
-                }
-#pragma unroll
-                for (int r = 0; r < R; ++r) d[r] = z[r] == kMinusInf ? (double)kMinusInf : d[r] + (double)b[r];
-                chosen = choose<R, double>(d, mine, k, g, group_values[wave], -1.0, near);
-            }
-        }
-
-        float part = 0.f;
-#pragma unroll
-        for (int r = 0; r < R; ++r) part += chosen >> r & 1 ? s[r] : 0.f;
-        const float sum = wave_sum(part);
-        int before = 0;
+    if (a.bias || (g.n > 1 && g.best == 2)) {
+        double c[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const bool on = chosen >> r & 1;
-            const unsigned long long all = __ballot(on);
-            if (on) {
-                const int e = r * 64 + lane, j = before + __popcll(all & ((1ull << lane) - 1));
-                const size_t at = (size_t)(t0 + t) * k + j;
-                const float w = !a.r.renorm ? s[r] : sum > 0.f ? s[r] / sum : 0.f;
-                a.ids[at] = e;
-                a.w[at] = w * a.r.scale;
-                chosen_ids[t * k + j] = (uint16_t)e;
-                atomicOr(&bits[e], (Bits)1 << t);
+            const double b = a.bias && mine >> r & 1 ? (double)clean(a.bias[r * 64 + lane]) : 0;
+            c[r] = z[r] == kMinusInf ? (double)kMinusInf : score(z[r]) + b;
+        }
+        chosen = choose<R, double>(c, mine, k, g, cl);
+    } else {
+        chosen = choose<R, float>(z, mine, k, g, reinterpret_cast<float *>(cl));
+    }
+    double part = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) part += chosen >> r & 1 ? score(z[r]) : 0;
+    const double sum = wave_sum(part);
+    int before = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const bool on = chosen >> r & 1;
+        const unsigned long long all = __ballot(on);
+        if (on) {
+            const int e = r * 64 + lane, j = before + __popcll(all & ((1ull << lane) - 1));
+            const double w = score(z[r]);
+            a.ids[t * k + j] = e;
+            a.w[t * k + j] = (float)(!a.r.renorm ? w : sum > 0 ? w / sum : 0) * a.r.scale;
+            chosen_ids[bit * k + j] = (uint16_t)e;
+            atomicOr(&bits[e], (Bits)1 << bit);
+        }
+        before += __popcll(all);
+    }
+}
+
+// ---- the fast way: four tokens per wave ------------------------------------------------------------------------------------
+
+// moves within 16 lanes in which every lane has a source
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xf, 0xf, true); }
+constexpr int kRor = 0x120;      // rotation: lane i gets lane i - n
+template <class Op>
+__device__ __forceinline__ uint32_t row_all(uint32_t x, Op op) {
+    x = op(x, dpp<kRor + 8>(x));
+    x = op(x, dpp<kRor + 4>(x));
+    x = op(x, dpp<kRor + 2>(x));
+    return op(x, dpp<kRor + 1>(x));
+}
+__device__ __forceinline__ uint32_t bits_of(float x) { return __builtin_bit_cast(uint32_t, x); }
+__device__ __forceinline__ float of_bits(uint32_t x) { return __builtin_bit_cast(float, x); }
+// maximum, minimum, sum over the 16 lanes of a token
+__device__ __forceinline__ uint32_t row_max(uint32_t x) { return row_all(x, [](uint32_t p, uint32_t q) { return max(p, q); }); }
+__device__ __forceinline__ float row_max(float x) { return of_bits(row_all(bits_of(x), [](uint32_t p, uint32_t q) { return bits_of(max_of(of_bits(p), of_bits(q))); })); }
+__device__ __forceinline__ float row_min(float x) { return of_bits(row_all(bits_of(x), [](uint32_t p, uint32_t q) { return bits_of(min_of(of_bits(p), of_bits(q))); })); }
+__device__ __forceinline__ float row_sum(float x) { return of_bits(row_all(bits_of(x), [](uint32_t p, uint32_t q) { return bits_of(of_bits(p) + of_bits(q)); })); }
+
+constexpr uint32_t kIndexBits = 511;      // low bits of a key: 511 - expert
+
+// Rows of logits (or the bias) come 16 neighbouring lanes after 16 neighbouring quads or elements, go through LDS, and are read
+// back V at a time: a lane that fetched its own V from memory would touch a line of its own with every load, and the address unit
+// takes a line at a time (64 tokens of 256 experts in one workgroup: 31 of 47 thousand cycles went into those loads).
+// Expert e lies at (e / V) * pitch + e % V; `pitch` keeps the lanes' reads on different banks.
+struct RowShape {
+    int E, V, pitch;
+    unsigned per_v;       // (e * per_v) >> 16 = e / V for e below 512
+    bool quads;           // four elements at a time: aligned, V and E multiples of four
+    __device__ __forceinline__ int at(int e) const {
+        const int l = (int)((unsigned)e * per_v >> 16);
+        return l * pitch + e - l * V;
+    }
+};
+template <int TYPE, int VT>
+__device__ __forceinline__ void fetch_row(const void *p, size_t row, const RowShape &r, int l, float (&z)[VT]) {
+    using T = std::conditional_t<TYPE == EF_F32, float, uint16_t>;
+    const T *x = static_cast<const T *>(p) + row;
+    if (r.quads) {
+        using T4 = std::conditional_t<TYPE == EF_F32, float4, ushort4>;
+        T4 q[VT / 4];
+#pragma unroll
+        for (int v = 0; v < VT / 4; ++v) q[v] = *reinterpret_cast<const T4 *>(x + min(64 * v + 4 * l, r.E - 4));
+#pragma unroll
+        for (int v = 0; v < VT / 4; ++v) {
+            z[4 * v] = value_of<TYPE>(q[v].x), z[4 * v + 1] = value_of<TYPE>(q[v].y);
+            z[4 * v + 2] = value_of<TYPE>(q[v].z), z[4 * v + 3] = value_of<TYPE>(q[v].w);
+        }
+    } else {
+        T h[VT];
+#pragma unroll
+        for (int v = 0; v < VT; ++v) h[v] = x[min(16 * v + l, r.E - 1)];
+#pragma unroll
+        for (int v = 0; v < VT; ++v) z[v] = value_of<TYPE>(h[v]);
+    }
+}
+template <int VT>
+__device__ __forceinline__ void fetch_row(const void *p, int type, size_t row, const RowShape &r, int l, float (&z)[VT]) {
+    if (type == EF_F32) fetch_row<EF_F32>(p, row, r, l, z);
+    else if (type == EF_BF16) fetch_row<EF_BF16>(p, row, r, l, z);
+    else fetch_row<EF_F16>(p, row, r, l, z);
+}
+template <int VT>
+__device__ __forceinline__ void put_row(float *to, const RowShape &r, int l, const float (&z)[VT]) {
+    if (r.quads) {
+#pragma unroll
+        for (int v = 0; v < VT / 4; ++v) {
+            const int e = 64 * v + 4 * l;
+            if (e < r.E) *reinterpret_cast<float4 *>(to + r.at(e)) = make_float4(clean(z[4 * v]), clean(z[4 * v + 1]), clean(z[4 * v + 2]), clean(z[4 * v + 3]));
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < VT; ++v) {
+            const int e = 16 * v + l;
+            if (e < r.E) to[r.at(e)] = clean(z[v]);
+        }
+    }
+}
+// this lane's V; what lies behind them is of no use
+template <int VT>
+__device__ __forceinline__ void get_row(const float *from, const RowShape &r, int l, float (&z)[VT]) {
+    if (r.quads) {
+#pragma unroll
+        for (int v = 0; v < VT; v += 4) {
+            const float4 q = *reinterpret_cast<const float4 *>(from + l * r.pitch + v);
+            z[v] = q.x, z[v + 1] = q.y, z[v + 2] = q.z, z[v + 3] = q.w;
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < VT; ++v) z[v] = from[l * r.pitch + v];
+    }
+}
+
+template <int TT> struct TileBits { using type = unsigned long long; };
+template <> struct TileBits<16> { using type = uint32_t; };
+
+// a tile of TT tokens per workgroup of NW waves, four tokens per wave at a time
+template <int VT, int TT, int NW>
+__global__ __launch_bounds__(64 * NW, VT <= 16 ? 4 : 2) void router_kernel(RouterArgs a, RowShape shape, bool fast) {
+    using Bits = typename TileBits<TT>::type;
+    constexpr int R = VT / 4, kE = 16 * VT, kThreads = 64 * NW;
+    constexpr int kRow = 16 * (VT + 4);
+    __shared__ Bits bits[kE], undecided;
+    __shared__ uint16_t chosen_ids[TT * EF_ROUTER_MAX_TOPK];
+    __shared__ int first[kE];
+    __shared__ __attribute__((aligned(16))) float rows[NW][4][kRow], bias[kRow];
+    static_assert(sizeof(rows[0]) >= kE * sizeof(double), "room for a token's values in 64 bits");
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int E = a.r.n_experts, k = a.r.top_k, V = shape.V;
+    const int t0 = blockIdx.x * TT, n = min(TT, a.T - t0);
+    float zn[VT];          // the next tokens' logits
+    const auto fetch = [&](int w0, int l) {
+        fetch_row<VT>(a.logits, a.type, (size_t)(t0 + min(w0 + (lane >> 4), n - 1)) * a.ld, shape, l, zn);
+    };
+    if (fast) fetch(wave * 4, lane & 15);
+    for (int e = tid; e < kE; e += kThreads) bits[e] = 0;
+    if (tid == 0) undecided = fast ? 0 : n == 8 * (int)sizeof(Bits) ? ~(Bits)0 : ((Bits)1 << n) - 1;
+    if (a.bias)
+        for (int e = tid; e < E; e += kThreads) bias[shape.at(e)] = clean(a.bias[e]);
+    __syncthreads();
+
+    const bool softmax = a.r.score == EF_SCORE_SOFTMAX;
+    const bool by_logit = !a.bias && (a.r.n_groups == 1 || a.r.group_best == 1);
+    for (int w0 = fast ? wave * 4 : n; w0 < n; w0 += NW * 4) {
+        // opaque: what follows from a lane's number is worked out in every pass instead of being kept, spilled, over all of them
+        int l = lane & 15;
+        asm volatile("" : "+v"(l));
+        const int e0 = l * V;
+        float *mine_rows = rows[wave][lane >> 4];
+        const int tok = w0 + (lane >> 4);
+        const size_t t = (size_t)t0 + min(tok, n - 1);
+        float c[VT], b[VT];     // logits, then choice values; bias
+        put_row<VT>(mine_rows, shape, l, zn);
+        if (TT > NW * 4 && w0 + NW * 4 < n) fetch(w0 + NW * 4, l);
+        wave_lds_sync();
+        get_row<VT>(mine_rows, shape, l, c);
+        if (a.bias) get_row<VT>(bias, shape, l, b);
+        else
+#pragma unroll
+            for (int v = 0; v < VT; ++v) b[v] = 0.f;
+        const int own = max(0, min(V, E - e0));      // experts of this lane
+        float m = kMinusInf;
+#pragma unroll
+        for (int v = 0; v < VT; ++v) {
+            c[v] = v < own ? c[v] : kMinusInf;
+            m = max_of(m, c[v]);
+        }
+        float top = 1.f, total = 0.f, bmax = 0.f;
+        if (softmax) {
+            m = row_max(m);
+            const float same = m > 0.f ? 0.f : kMinusInf;     // for inf - inf, and -inf - -inf
+            float x[VT];
+#pragma unroll
+            for (int v = 0; v < VT; ++v) {
+                const float d = c[v] - m;
+                x[v] = pinned(__expf(d != d ? same : d));
+                total += x[v];
             }
-            before += __popcll(all);
+            total = row_sum(total);
+            top = total > 0.f ? 1.f / total : 0.f;
+            if (!by_logit)
+#pragma unroll
+                for (int v = 0; v < VT; ++v) c[v] = c[v] == kMinusInf ? kMinusInf : x[v] * top;
+        } else if (!by_logit) {
+#pragma unroll
+            for (int v = 0; v < VT; ++v) {
+                const float s = pinned(__builtin_amdgcn_rcpf(1.f + __expf(-c[v])));
+                c[v] = c[v] == kMinusInf ? kMinusInf : s;
+            }
+        }
+        if (!by_logit) {
+#pragma unroll
+            for (int v = 0; v < VT; ++v) {
+                bmax = max_of(bmax, v < own && fabsf(b[v]) < __builtin_inff() ? fabsf(b[v]) : 0.f);
+                c[v] = c[v] == kMinusInf ? kMinusInf : c[v] + b[v];
+            }
+            bmax = row_max(bmax);
+        }
+        // A choice value is off by at most 5e-7 (sigmoid: exp, sum, reciprocal) or 1.6e-6 (softmax: the sum's error too) of the
+        // largest score and 2^-24 of itself, a sum of two by twice that; a margin is two such errors.
+        const float margin = by_logit ? -1.f : (softmax ? 8e-6f : 2.5e-6f) * top + 1e-6f * bmax;
+
+        bool near = false, kept = true;
+        if (a.r.n_groups > 1) {
+            const int P = 16 / a.r.n_groups;     // lanes of a group
+            float b1 = kMinusInf, b2 = kMinusInf;
+#pragma unroll
+            for (int v = 0; v < VT; ++v) {
+                b2 = __builtin_amdgcn_fmed3f(b1, b2, c[v]);
+                b1 = max_of(b1, c[v]);
+            }
+            const auto join = [&](uint32_t o1b, uint32_t o2b) {
+                const float o1 = of_bits(o1b), o2 = of_bits(o2b);
+                b2 = fmaxf(fminf(b1, o1), fmaxf(b2, o2));
+                b1 = fmaxf(b1, o1);
+            };
+            if (P >= 2) join(dpp<0xB1>(bits_of(b1)), dpp<0xB1>(bits_of(b2)));         // lanes in pairs,
+            if (P >= 4) join(dpp<0x4E>(bits_of(b1)), dpp<0x4E>(bits_of(b2)));         // fours,
+            if (P >= 8) join(dpp<0x141>(bits_of(b1)), dpp<0x141>(bits_of(b2)));       // eights (mirrored)
+            const float value = a.r.group_best == 1 ? b1 : b2 == kMinusInf ? kMinusInf : b1 + b2;
+            int rank = 0;
+            const auto rank_groups = [&](auto lanes) {      // a lane of every other group; a lower lane is of a lower group
+                constexpr int p = decltype(lanes)::value;
+                static_for<1, 16 / p>([&](auto o) {
+                    const float ov = of_bits(dpp<kRor + decltype(o)::value * p>(bits_of(value)));
+                    rank += l >= decltype(o)::value * p ? ov >= value : ov > value;
+                });
+            };
+            if (P == 1) rank_groups(std::integral_constant<int, 1>{});
+            else if (P == 2) rank_groups(std::integral_constant<int, 2>{});
+            else if (P == 4) rank_groups(std::integral_constant<int, 4>{});
+            else rank_groups(std::integral_constant<int, 8>{});
+            kept = rank < a.r.groups_kept;
+            if (a.r.groups_kept < a.r.n_groups && margin >= 0.f) {
+                const float worst = row_min(kept ? value : __builtin_inff()), best = row_max(kept ? kMinusInf : value);
+                near = worst - best <= margin;
+            }
+        }
+        uint32_t key[VT];
+        const int live = kept ? own : 0;
+#pragma unroll
+        for (int v = 0; v < VT; ++v) key[v] = v < live ? (key_of(c[v]) & ~kIndexBits) | (kIndexBits - (uint32_t)(e0 + v)) : 0u;
+        const auto below = [&](uint32_t last) {     // the largest key below `last`
+            uint32_t d = key[0] - last;
+#pragma unroll
+            for (int v = 1; v < VT; ++v) d = max(d, key[v] - last);
+            return row_max(d) + last;
+        };
+        uint32_t prev = 0, last = 0, won = 0;
+        for (int j = 0; j < k; ++j) {
+            prev = last;
+            last = below(last);
+            if (l == j) won = last;
+        }
+        if (a.type == EF_F32 || !by_logit) {
+            // the keys' upper bits hold a value to 2^-14 of itself: the best expert left out may be ahead of the last one chosen.
+            // Where no third one is as close, their values in full decide between the two
+            const uint32_t next = below(last);
+            const auto close = [&](uint32_t hi, uint32_t lo) {      // 0 and what below() gives behind the last key are not values
+                const float x = of_key(hi & ~kIndexBits), y = of_key(lo & ~kIndexBits);
+                return lo > kIndexBits && lo < hi && (((hi ^ lo) & ~kIndexBits) == 0 || x - y <= margin + 0x1p-14f * (fabsf(x) + fabsf(y)));
+            };
+            const bool border = close(last, next);
+            if (__ballot(border)) {
+                const uint32_t third = below(next);
+                if (border) {
+                    near |= (k > 1 && close(prev, last)) || (next < last && close(next, third));
+                    const int ea = (int)(kIndexBits - (last & kIndexBits)), eb = (int)(kIndexBits - (next & kIndexBits));
+                    const float za = mine_rows[shape.at(ea)], zb = mine_rows[shape.at(eb)];
+                    const auto choice = [&](float z, int e) {
+                        if (by_logit || z == kMinusInf) return z;
+                        const float d = z - m;
+                        const float s = softmax ? __expf(d != d ? 0.f : d) * top : __builtin_amdgcn_rcpf(1.f + __expf(-z));
+                        return a.bias ? s + bias[shape.at(e)] : s;
+                    };
+                    const float ca = choice(za, ea), cb = choice(zb, eb);
+                    if (!by_logit) near |= fabsf(ca - cb) <= margin;
+                    if (cb > ca || (cb == ca && eb < ea)) {
+                        if (l == k - 1) won = next;
+                    }
+                }
+            }
+        }
+        if (tok < n && near && l == 0) atomicOr(&undecided, (Bits)1 << tok);
+        // lanes 0..k-1: one chosen expert each, its place among them, its score
+        const bool mine = l < k && tok < n && !near;
+        const int e = (int)(kIndexBits - (won & kIndexBits));
+        int place = 0;
+        static_for<1, 16>([&](auto o) { place += dpp<kRor + decltype(o)::value>(l < k ? (uint32_t)e : 1u << 16) < (uint32_t)e; });
+        float w = 0.f;
+        if (mine) {
+            const float z = mine_rows[shape.at(e)];
+            w = !softmax ? 1.f / (1.f + expf(-z)) : z == kMinusInf ? 0.f : z == m ? top : expf(z - m) * top;
+        }
+        if (a.r.renorm) {
+            const float sum = row_sum(w);
+            w = sum > 0.f ? w / sum : 0.f;
+        }
+        if (mine) {
+            a.ids[t * k + place] = e;
+            a.w[t * k + place] = w * a.r.scale;
+            chosen_ids[tok * k + place] = (uint16_t)e;
+            atomicOr(&bits[e], (Bits)1 << tok);
         }
     }
     __syncthreads();
+    if (undecided) {       // uniform; a wave per token
+        Groups g{a.r.n_groups, E / a.r.n_groups, a.r.groups_kept, a.r.group_best, 64};
+        while (g.lanes * g.n > 64) g.lanes >>= 1;
+        int nth = 0;
+        for (Bits todo = undecided; todo; todo &= todo - 1, ++nth)
+            if (nth % NW == wave) {
+                const int x = __builtin_ctzll(todo);
+                exact_token<R>(a, (size_t)t0 + x, x, g, reinterpret_cast<double *>(&rows[wave][0][0]), chosen_ids, bits);
+                wave_lds_sync();
+            }
+        __syncthreads();
+    }
 
     if (a.ntiles > 1) {
-        for (int e = tid; e < E; e += 64 * kRouterWaves) a.tile_counts[(size_t)e * a.ntiles + blockIdx.x] = __popcll(bits[e]);
-        for (int x = tid; x < n * k; x += 64 * kRouterWaves)
+        for (int e = tid; e < a.pitch; e += kThreads) a.tile_counts[(size_t)blockIdx.x * a.pitch + e] = (uint8_t)__popcll(bits[e]);
+        for (int x = tid; x < n * k; x += kThreads)
             a.rank[(size_t)t0 * k + x] = (uint8_t)__popcll(bits[chosen_ids[x]] & (((Bits)1 << (x / k)) - 1));
         return;
     }
@@ -342,7 +582,7 @@ __global__ __launch_bounds__(64 * kRouterWaves) void router_kernel(RouterArgs a)
         if (lane == 0) a.offsets[E] = all;
     }
     __syncthreads();
-    for (int x = tid; x < n * k; x += 64 * kRouterWaves) {
+    for (int x = tid; x < n * k; x += kThreads) {
         const int e = chosen_ids[x];
         const int pos = first[e] + __popcll(bits[e] & (((Bits)1 << (x / k)) - 1));
         a.perm[pos] = x;
@@ -350,41 +590,75 @@ __global__ __launch_bounds__(64 * kRouterWaves) void router_kernel(RouterArgs a)
     }
 }
 
-// the tiles' counts of an expert -> their exclusive prefix, in place, and the expert's total; a wave per expert
-__global__ __launch_bounds__(256) void router_scan_kernel(int32_t *__restrict__ tile_counts, int ntiles, int E, int32_t *__restrict__ counts) {
-    const int e = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (e >= E) return;
-    int32_t *row = tile_counts + (size_t)e * ntiles;
-    int before = 0;
-    for (int c0 = 0; c0 < ntiles; c0 += 64) {
-        const int v = c0 + lane < ntiles ? row[c0 + lane] : 0;
-        int incl = v;
+// Adds up the tiles' counts of every expert, over all tiles and over those before `tile`.  A thread takes 16 experts of every
+// (256 / threads per tile)-th tile, eight loads of 16 bytes in flight, and adds the bytes in pairs of 16 bits, which hold the sum
+// of its tiles.
+template <int R>
+__device__ __forceinline__ void add_counts(const RouterArgs &a, int tile, int *total, int *before) {
+    constexpr int kPer = 4 * R, kStep = 256 / kPer;      // threads per tile, tiles per round
+    static_assert(kRouterSumTiles / kStep * 64 < 65536, "16 bits per sum");
+    const int tid = threadIdx.x, sixteen = tid % kPer;
+    for (int e = tid; e < 64 * R; e += 256) total[e] = before[e] = 0;
+    __syncthreads();
+    const uint4 *counts = reinterpret_cast<const uint4 *>(a.tile_counts) + sixteen;
+    const auto add = [&](int b0, int b1, int *to, int *and_to) {
+        uint32_t even[4] = {0, 0, 0, 0}, odd[4] = {0, 0, 0, 0};
+        for (int b = b0 + tid / kPer; b < b1; b += kStep * 8) {
+            uint4 x[8];
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(incl, o);
-            if (lane >= o) incl += x;
+            for (int i = 0; i < 8; ++i) x[i] = counts[(size_t)min(b + i * kStep, b1 - 1) * (a.pitch / 16)];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t mask = b + i * kStep < b1 ? 0x00FF00FFu : 0u, w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    even[q] += w[q] & mask;
+                    odd[q] += w[q] >> 8 & mask;
+                }
+            }
         }
-        if (c0 + lane < ntiles) row[c0 + lane] = before + incl - v;
-        before += __shfl(incl, 63);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int x = (i & 1 ? odd[i >> 2] : even[i >> 2]) >> (i & 2 ? 16 : 0) & 0xFFFF;
+            if (x) {
+                atomicAdd(to + sixteen * 16 + i, x);
+                if (and_to) atomicAdd(and_to + sixteen * 16 + i, x);
+            }
+        }
+    };
+    if (sixteen * 16 < a.pitch) {
+        add(0, tile, before, total);
+        add(tile, a.ntiles, total, nullptr);
     }
-    if (lane == 0) counts[e] = before;
+    __syncthreads();
 }
 
+// scatter of a tile; `scanned`: the prefixes over the tiles and the totals are there already
 template <int R>
-__global__ __launch_bounds__(256) void router_scatter_kernel(RouterArgs a, int tile) {
-    __shared__ int first[64 * R];
+__global__ __launch_bounds__(256) void router_scatter_kernel(RouterArgs a, int tile, bool scanned) {
+    __shared__ int first[64 * R], total[64 * R];
     const int E = a.r.n_experts, k = a.r.top_k, tid = threadIdx.x, lane = tid & 63;
+    if (scanned) {
+        for (int e = tid; e < 64 * R; e += 256) {
+            total[e] = e < E ? a.counts[e] : 0;
+            first[e] = e < E ? a.prefix[(size_t)blockIdx.x * a.pitch + e] : 0;
+        }
+        __syncthreads();
+    } else {
+        add_counts<R>(a, blockIdx.x, total, first);
+    }
     if (tid < 64) {
         int cnt[R], off[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) cnt[r] = r * 64 + lane < E ? a.counts[r * 64 + lane] : 0;
+        for (int r = 0; r < R; ++r) cnt[r] = total[r * 64 + lane];
         const int all = expert_offsets<R>(cnt, off);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int e = r * 64 + lane;
-            if (e < E) {
-                first[e] = off[r] + a.tile_counts[(size_t)e * a.ntiles + blockIdx.x];
-                if (blockIdx.x == 0) a.offsets[e] = off[r];
+            first[e] += off[r];
+            if (blockIdx.x == 0 && e < E) {
+                a.offsets[e] = off[r];
+                if (!scanned) a.counts[e] = cnt[r];
             }
         }
         if (blockIdx.x == 0 && lane == 0) a.offsets[E] = all;
@@ -399,15 +673,44 @@ __global__ __launch_bounds__(256) void router_scatter_kernel(RouterArgs a, int t
     }
 }
 
-template <int R>
-hipError_t launch_r(const RouterArgs &a, hipStream_t s) {
-    const int tile = router_tile(a.T);
-    if (tile == 16) hipLaunchKernelGGL((router_kernel<R, 16>), dim3(a.ntiles), dim3(64 * kRouterWaves), 0, s, a);
-    else hipLaunchKernelGGL((router_kernel<R, 64>), dim3(a.ntiles), dim3(64 * kRouterWaves), 0, s, a);
+// many tiles: their counts' exclusive prefixes, an expert per workgroup of 256
+__global__ __launch_bounds__(256) void router_scan_kernel(RouterArgs a) {
+    __shared__ int part[256];
+    const int e = blockIdx.x, tid = threadIdx.x, per = (a.ntiles + 255) / 256;
+    const int b0 = min(a.ntiles, tid * per), b1 = min(a.ntiles, b0 + per);
+    int sum = 0;
+    for (int b = b0; b < b1; ++b) sum += a.tile_counts[(size_t)b * a.pitch + e];
+    part[tid] = sum;
+    __syncthreads();
+    int before = 0, all = 0;
+    for (int i = 0; i < 256; ++i) {
+        before += i < tid ? part[i] : 0;
+        all += part[i];
+    }
+    for (int b = b0; b < b1; ++b) {
+        a.prefix[(size_t)b * a.pitch + e] = before;
+        before += a.tile_counts[(size_t)b * a.pitch + e];
+    }
+    if (tid == 0) a.counts[e] = all;
+}
+
+template <int VT>
+hipError_t launch_v(const RouterArgs &a, hipStream_t s) {
+    const int tile = router_tile(a.T), E = a.r.n_experts, V = (E + 15) / 16;
+    const bool fast = a.r.n_groups == 1 || (E % 16 == 0 && 16 % a.r.n_groups == 0);
+    const size_t size = a.type == EF_F32 ? 4 : 2;
+    const bool quads = V % 4 == 0 && E % 4 == 0 && a.ld % 4 == 0 && reinterpret_cast<size_t>(a.logits) % (4 * size) == 0 &&
+                       reinterpret_cast<size_t>(a.bias) % 16 == 0;
+    const RowShape shape{E, V, quads ? V + 4 : V | 1, (65536u + V - 1) / V, quads};
+    // one tile: a wave for every four tokens; many: two passes per wave, so that two workgroups fit a compute unit's LDS
+    if (tile == 16) hipLaunchKernelGGL((router_kernel<VT, 16, 4>), dim3(a.ntiles), dim3(256), 0, s, a, shape, fast);
+    else if (a.ntiles == 1) hipLaunchKernelGGL((router_kernel<VT, 64, 16>), dim3(1), dim3(1024), 0, s, a, shape, fast);
+    else hipLaunchKernelGGL((router_kernel<VT, 64, 8>), dim3(a.ntiles), dim3(512), 0, s, a, shape, fast);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.ntiles == 1) return e;
-    hipLaunchKernelGGL(router_scan_kernel, dim3((a.r.n_experts + 3) / 4), dim3(256), 0, s, a.tile_counts, a.ntiles, a.r.n_experts, a.counts);
-    hipLaunchKernelGGL(router_scatter_kernel<R>, dim3(a.ntiles), dim3(256), 0, s, a, tile);
+    const bool scan = a.prefix != nullptr;
+    if (scan) hipLaunchKernelGGL(router_scan_kernel, dim3(E), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((router_scatter_kernel<VT / 4>), dim3(a.ntiles), dim3(256), 0, s, a, tile, scan);
     return hipGetLastError();
 }
 
@@ -422,8 +725,8 @@ hipError_t launch_router(const RouterArgs &a, hipStream_t s) {
         const hipError_t e = launch_fill_i32(a.counts, E, 0, s);
         return e != hipSuccess ? e : launch_fill_i32(a.offsets, E + 1, 0, s);
     }
-    if (a.ntiles != (a.T + router_tile(a.T) - 1) / router_tile(a.T)) return hipErrorInvalidValue;
-    return E <= 64 ? launch_r<1>(a, s) : E <= 128 ? launch_r<2>(a, s) : E <= 256 ? launch_r<4>(a, s) : launch_r<8>(a, s);
+    if (a.ntiles != (a.T + router_tile(a.T) - 1) / router_tile(a.T) || a.pitch < E || a.pitch % 4 != 0) return hipErrorInvalidValue;
+    return E <= 64 ? launch_v<4>(a, s) : E <= 128 ? launch_v<8>(a, s) : E <= 256 ? launch_v<16>(a, s) : launch_v<32>(a, s);
 }
 
 }  // namespace ef

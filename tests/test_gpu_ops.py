@@ -81,6 +81,10 @@ ROUTES = [
     (1000, 60, 4, "bf16", dict(renorm=True)), (9000, 128, 6, "f16", dict(sigmoid=True, n_groups=4, groups_kept=2)),
     (70, 512, 16, "f32", dict(n_groups=2, groups_kept=1)), (40, 34, 3, "f32", dict(n_groups=17, groups_kept=2, group_best=2, sigmoid=True)),
     (8193, 8, 2, "f32", dict(renorm=True)),
+    # more tiles than a workgroup adds up by itself; rows and shapes of every way to load and to share groups
+    (66000, 20, 3, "bf16", dict(renorm=True)), (77, 48, 4, "f16", dict(sigmoid=True, n_groups=16, groups_kept=7)),
+    (50, 64, 16, "bf16", dict(n_groups=2, groups_kept=2, group_best=2)), (30, 256, 8, "bf16", dict(renorm=True)),
+    (21, 496, 16, "f16", dict(sigmoid=True, n_groups=8, groups_kept=3, group_best=2)),
 ]
 
 
