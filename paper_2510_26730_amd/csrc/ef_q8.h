@@ -116,9 +116,15 @@ __device__ __forceinline__ void q8_put4(char *row, int c, int type, const float 
     }
 }
 
-// columns n .. n+3 of an output row, as far as they are below n_end
+// columns n .. n+3 of an output row, as far as they are below n_end: one store where the four are there and aligned
 __device__ __forceinline__ void q8_store4(const Q8Args &p, int row, int n, int n_end, const float (&v)[4]) {
     const size_t at = (size_t)row * p.ldo + n;
+    const int size = p.out_type == EF_F32 ? 4 : 2;
+    char *to = static_cast<char *>(p.out) + at * size;
+    if (n + 4 <= n_end && (reinterpret_cast<size_t>(to) & (4 * size - 1)) == 0) {
+        q8_put4(to, 0, p.out_type, v);
+        return;
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         if (n + e >= n_end) return;

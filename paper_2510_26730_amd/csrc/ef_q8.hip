@@ -178,117 +178,172 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(QuantArgs a) {
 typedef int int4v __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ int4v load16(const int8_t *p) { return *reinterpret_cast<const int4v *>(p); }
-__device__ __forceinline__ int4v load16_stream(const int8_t *p) { return __builtin_nontemporal_load(reinterpret_cast<const int4v *>(p)); }
 
-// A wave: 32 columns of the matrix (swiglu: 16 gate and their 16 up columns) for TT tiles of 16 rows, K in KS parts over the
-// waves of a workgroup, which are added in LDS.
-constexpr int kStreamDepth = 4;    // K steps of 64 in flight per wave
+// A wave: NB blocks of 16 matrix rows (swiglu: 16 gate and their 16 up rows) for TT tiles of 16 product rows, in steps of 128 codes,
+// DEPTH steps in flight; K in KS parts over the waves of a workgroup, which are added in LDS.
+//
+// A load of a wave takes 8 rows x 128 bytes, whole lines: lane 8c + r gets chunk c (16 bytes) of row r, or of row 8 + r in the second
+// load.  The matrix instruction wants row i in the lanes i, i + 16, i + 32, i + 48, so the halves of 16 lanes swap: of the first load
+// the upper half (odd chunks of rows 0..7) against the lower half of the second one (even chunks of rows 8..15).  Then every lane has
+// chunks 2g and 2g + 1 of its own row.  Loads of 16 rows x 64 bytes, which need no swap, were slower: MEASURED_STREAM.
+__device__ __forceinline__ void swap_halves(int4v &lo, int4v &hi, bool upper) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int away = upper ? lo[e] : hi[e];
+        const int back = __builtin_amdgcn_mov_dpp(away, 0x128, 0xf, 0xf, true);   // 16 lanes rotated by 8
+        lo[e] = upper ? back : lo[e];
+        hi[e] = upper ? hi[e] : back;
+    }
+}
 
-template <int TT, bool PAIR, int KS>
-__global__ __launch_bounds__(256) void q8_stream_kernel(Q8Args p) {
-    __shared__ int4v sums[KS > 1 ? 4 : 1][2 * TT][64];
+template <int TT, bool PAIR, int NB, int KS, int DEPTH>
+__global__ __launch_bounds__(64 * (KS > 4 ? KS : 4)) void q8_stream_kernel(Q8Args p) {
+    static_assert(!PAIR || NB == 2, "gate and up");
+    constexpr int kWaves = KS > 4 ? KS : 4;
+    __shared__ int4v sums[KS > 1 ? kWaves : 1][NB * TT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Q8Tile t;
     if (!q8_find_tile(p, blockIdx.y, 16 * TT, t)) return;
     const int part = wave & (KS - 1), cw = wave / KS;
     const int F = p.N >> 1;
-    const int n0 = (blockIdx.x * (4 / KS) + cw) * (PAIR ? 16 : 32), n_end = PAIR ? F : p.N;
+    const int n0 = (blockIdx.x * (kWaves / KS) + cw) * (PAIR ? 16 : 16 * NB), n_end = PAIR ? F : p.N;
     const int i = lane & 15, g = lane >> 4;
-    const int steps = (p.K + 63) >> 6;
+    const int steps = (p.K + 127) >> 7;
     const int s0 = steps * part / KS, s1 = steps * (part + 1) / KS;
+    const bool run = n0 < n_end && s0 < s1;
 
     // columns past the end and rows past the group's read a neighbour's codes; their results are dropped
-    const int c0 = min(n0 + i, n_end - 1), c1 = PAIR ? F + c0 : min(n0 + 16 + i, n_end - 1);
-    const int8_t *w = p.w + (size_t)t.group * p.w_group;
-    const int8_t *w0 = w + (size_t)c0 * p.ldw, *w1 = w + (size_t)c1 * p.ldw;
-    const int8_t *x[TT];
-    float xs[TT];
+    const int8_t *w[NB][2];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int c = min(n0 + (PAIR ? 0 : 16 * b) + 8 * h + (lane & 7), n_end - 1);
+            w[b][h] = p.w + (size_t)t.group * p.w_group + (size_t)(PAIR && b ? F + c : c) * p.ldw;
+        }
+    const int k_last = ((p.K + 15) & ~15) - 16;   // last 16 codes that a weight row holds
+    int4v wb[NB][2][DEPTH], xb[TT][2][DEPTH];
+    const auto fetch_w = [&](int u, int s) {
+        const int k = min(min(s, s1 - 1) * 128 + 16 * (lane >> 3), k_last);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) wb[b][h][u] = load16(w[b][h] + k);
+    };
+    if (run)
+#pragma unroll
+        for (int u = 0; u < DEPTH; ++u) fetch_w(u, s0 + u);
+
+    const int8_t *x[TT][2];
+    float xs[TT], ws[NB][4];
 #pragma unroll
     for (int j = 0; j < TT; ++j) {
-        const Q8Row r = q8_row(p, min(t.row0 + 16 * j + i, t.row_end - 1));
-        x[j] = p.a + (size_t)r.row * p.lda + 16 * g;
-        xs[j] = r.scale;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) x[j][h] = p.a + (size_t)q8_row(p, min(t.row0 + 16 * j + 8 * h + (lane & 7), t.row_end - 1)).row * p.lda;
+        xs[j] = q8_row(p, min(t.row0 + 16 * j + i, t.row_end - 1)).scale;
     }
-    const int k_last = ((p.K + 15) & ~15) - 16;   // last 16 codes that a weight row holds; beyond K the rows of `a` are zero
-
-    int4v acc[2][TT];
 #pragma unroll
-    for (int j = 0; j < TT; ++j) acc[0][j] = acc[1][j] = int4v{0, 0, 0, 0};
-    int4v wb[2][kStreamDepth], xb[TT][kStreamDepth];
-    const auto fetch = [&](int u, int s) {
-        const int k = min(s, s1 - 1) * 64;
-        const int kw = min(k + 16 * g, k_last);
-        wb[0][u] = load16_stream(w0 + kw);
-        wb[1][u] = load16_stream(w1 + kw);
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int j = 0; j < TT; ++j) xb[j][u] = load16(x[j] + k);
-    };
-    if (n0 < n_end && s0 < s1) {
-#pragma unroll
-        for (int u = 0; u < kStreamDepth; ++u) fetch(u, s0 + u);
-        for (int s = s0; s < s1; s += kStreamDepth) {
-#pragma unroll
-            for (int u = 0; u < kStreamDepth; ++u) {
-                if (s + u < s1) {
-#pragma unroll
-                    for (int j = 0; j < TT; ++j) {
-                        acc[0][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wb[0][u], xb[j][u], acc[0][j], 0, 0, 0);
-                        acc[1][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wb[1][u], xb[j][u], acc[1][j], 0, 0, 0);
-                    }
-                }
-                fetch(u, s + u + kStreamDepth);
-            }
+        for (int e = 0; e < 4; ++e) {
+            const int c = min(n0 + (PAIR ? 0 : 16 * b) + 4 * g + e, n_end - 1);
+            ws[b][e] = p.w_scale[(size_t)t.group * p.N + (PAIR && b ? F + c : c)];
         }
-    }
-    if constexpr (KS > 1) {
-#pragma unroll
-        for (int j = 0; j < TT; ++j) {
-            sums[wave][2 * j][lane] = acc[0][j];
-            sums[wave][2 * j + 1][lane] = acc[1][j];
-        }
-        __syncthreads();
-        if (part != 0) return;
+    // Rows of `a` are zero from K up to x_end, a multiple of 64; chunks behind it are read from before it and cleared
+    const int x_end = (p.K + 63) & ~63;
+    const auto fetch_x = [&](int u, int s) {
+        const int k = min(min(s, s1 - 1) * 128 + 16 * (lane >> 3), x_end - 16);
 #pragma unroll
         for (int j = 0; j < TT; ++j)
 #pragma unroll
-            for (int q = 1; q < KS; ++q) {
-                acc[0][j] += sums[wave + q][2 * j][lane];
-                acc[1][j] += sums[wave + q][2 * j + 1][lane];
+            for (int h = 0; h < 2; ++h) xb[j][h][u] = load16(x[j][h] + k);
+    };
+
+    int4v acc[NB][TT];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int j = 0; j < TT; ++j) acc[b][j] = int4v{0, 0, 0, 0};
+    if (run) {
+#pragma unroll
+        for (int u = 0; u < DEPTH; ++u) fetch_x(u, s0 + u);
+        const bool upper = lane & 8;
+        const auto multiply = [&](int u, int s) {
+#pragma unroll
+            for (int j = 0; j < TT; ++j) swap_halves(xb[j][0][u], xb[j][1][u], upper);
+            if (s * 128 + 128 > x_end && g >= 2) {
+#pragma unroll
+                for (int j = 0; j < TT; ++j) xb[j][0][u] = xb[j][1][u] = int4v{0, 0, 0, 0};
             }
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                swap_halves(wb[b][0][u], wb[b][1][u], upper);
+#pragma unroll
+                for (int j = 0; j < TT; ++j) {
+                    acc[b][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wb[b][0][u], xb[j][0][u], acc[b][j], 0, 0, 0);
+                    acc[b][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wb[b][1][u], xb[j][1][u], acc[b][j], 0, 0, 0);
+                }
+            }
+        };
+        // loads without a branch between them keep the compiler's wait counts exact; past the end they repeat the last step
+        int s = s0;
+        for (; s + DEPTH < s1; s += DEPTH) {
+#pragma unroll
+            for (int u = 0; u < DEPTH; ++u) {
+                multiply(u, s + u);
+                fetch_w(u, s + u + DEPTH);
+                fetch_x(u, s + u + DEPTH);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < DEPTH; ++u)
+            if (s + u < s1) multiply(u, s + u);
+    }
+    if constexpr (KS > 1) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int j = 0; j < TT; ++j) sums[wave][b * TT + j][lane] = acc[b][j];
+        __syncthreads();
+        if (part != 0) return;
+#pragma unroll
+        for (int q = 1; q < KS; ++q)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int j = 0; j < TT; ++j) acc[b][j] += sums[wave + q][b * TT + j][lane];
     }
     if (n0 >= n_end) return;
-    // lane 16g + i holds row (token) i, columns 4g .. 4g+3 of each 16
-    const float *ws = p.w_scale + (size_t)t.group * p.N;
+    // lane 16g + i holds product row i, matrix rows 4g .. 4g+3 of each 16
 #pragma unroll
     for (int j = 0; j < TT; ++j) {
         const int row = t.row0 + 16 * j + i;
         if (row >= t.row_end) continue;
-        if constexpr (PAIR) {
-            float v[4];
+        float v[NB][4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int f = min(n0 + 4 * g + e, F - 1);
-                v[e] = silu_mul((float)acc[0][j][e] * xs[j] * ws[f], (float)acc[1][j][e] * xs[j] * ws[F + f]);
-            }
-            q8_store4(p, row, n0 + 4 * g, F, v);
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[b][e] = (float)acc[b][j][e] * xs[j] * ws[b][e];
+        if constexpr (PAIR) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[0][e] = silu_mul(v[0][e], v[1][e]);
+            q8_store4(p, row, n0 + 4 * g, n_end, v[0]);
         } else {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                float v[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = (float)acc[h][j][e] * xs[j] * ws[min(n0 + 16 * h + 4 * g + e, p.N - 1)];
-                q8_store4(p, row, n0 + 16 * h + 4 * g, p.N, v);
-            }
+            for (int b = 0; b < NB; ++b) q8_store4(p, row, n0 + 16 * b + 4 * g, n_end, v[b]);
         }
     }
 }
 
 template <int TT, bool PAIR>
 hipError_t launch_stream(const Q8Args &p, hipStream_t s) {
-    const int per_wave = PAIR ? 16 : 32, cols = PAIR ? p.N / 2 : p.N;
-    const int waves = (cols + per_wave - 1) / per_wave, tiles = q8_tiles_bound(p, 16 * TT);
-    if ((long long)waves * tiles >= 2048) hipLaunchKernelGGL((q8_stream_kernel<TT, PAIR, 1>), dim3((waves + 3) / 4, tiles), dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((q8_stream_kernel<TT, PAIR, 4>), dim3(waves, tiles), dim3(256), 0, s, p);
+    const int cols = PAIR ? p.N / 2 : p.N, tiles = q8_tiles_bound(p, 16 * TT);
+    const int b16 = (cols + 15) / 16, b32 = (cols + 31) / 32, wide = PAIR ? b16 : b32;   // waves per tile without a split of K
+    if (tiles > 65535) return hipErrorInvalidValue;
+    const long long waves = (long long)wide * tiles;
+    if (waves >= 2048) hipLaunchKernelGGL((q8_stream_kernel<TT, PAIR, 2, 1, 1>), dim3((wide + 3) / 4, tiles), dim3(256), 0, s, p);
+    else if (PAIR || TT > 1 || waves >= 512) hipLaunchKernelGGL((q8_stream_kernel<TT, PAIR, 2, 4, 2>), dim3(wide, tiles), dim3(256), 0, s, p);
+    else if constexpr (!PAIR && TT == 1) hipLaunchKernelGGL((q8_stream_kernel<1, false, 1, 8, 4>), dim3(b16, tiles), dim3(512), 0, s, p);
     return hipGetLastError();
 }
 
