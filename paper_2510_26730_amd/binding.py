@@ -9,6 +9,7 @@ a missing library is an error, there is no fallback.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -190,13 +191,14 @@ def _ptr(x):
     """Address of a torch tensor / numpy array / raw int / None."""
     if x is None:
         return None
+    address = getattr(x, "data_ptr", None)
+    if address is not None:
+        assert x.is_contiguous()
+        return address()
     if isinstance(x, int):
         return x
-    if isinstance(x, np.ndarray):
-        assert x.flags["C_CONTIGUOUS"]
-        return x.ctypes.data
-    assert x.is_contiguous()
-    return x.data_ptr()
+    assert x.flags["C_CONTIGUOUS"]
+    return x.ctypes.data
 
 
 def _check(ctx, rc):
@@ -575,21 +577,30 @@ def ef_delta_assemble(c, token_ids, tok_off, layer, S, H, L, gain, M, out=None):
 # ---- operators beside the layer ------------------------------------------------------------------
 # Two-dimensional operands may have any row stride; their elements of a row are consecutive.
 
+_kinds = {}
+
+
 def _rows(x):
     """(address, type, elements from row to row) of a matrix of tensor rows."""
-    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
-        raise EfError(EF_EINVAL, "a matrix with consecutive row elements is needed")
-    name = str(x.dtype)
-    kind = {"torch.bfloat16": EF_BF16, "torch.float16": EF_F16, "torch.float32": EF_F32, "torch.int8": EF_I8}.get(name)
+    if not _kinds:
+        import torch
+        _kinds.update({torch.bfloat16: EF_BF16, torch.float16: EF_F16, torch.float32: EF_F32, torch.int8: EF_I8})
+    kind = _kinds.get(x.dtype)
     if kind is None:
-        raise EfError(EF_EINVAL, f"unsupported element type {name}")
-    return x.data_ptr(), kind, x.stride(0) if x.shape[0] > 1 else max(x.stride(0), x.shape[1])
+        raise EfError(EF_EINVAL, f"unsupported element type {x.dtype}")
+    if x.dim() != 2:
+        raise EfError(EF_EINVAL, "a matrix is needed")
+    (rows, cols), (ld, step) = x.shape, x.stride()
+    if cols > 1 and step != 1:
+        raise EfError(EF_EINVAL, "a matrix with consecutive row elements is needed")
+    return x.data_ptr(), kind, ld if rows > 1 else max(ld, cols)
 
 
 def _work(work):
-    return (None, 0) if work is None else (_ptr(work), work.numel() * work.element_size())
+    return (None, 0) if work is None else (_ptr(work), work.nbytes)
 
 
+@functools.lru_cache(maxsize=256)
 def _router(E, k, sigmoid, n_groups, groups_kept, group_best, renorm, scale):
     return ef_router(E, k, EF_SCORE_SIGMOID if sigmoid else EF_SCORE_SOFTMAX, n_groups, groups_kept, group_best, int(renorm), scale)
 
@@ -623,24 +634,23 @@ def ef_quant_rows(x, codes, scales, stream=None):
 
 
 def _product(a, w, w_scale, out, a_scale, rows, row_div, offsets, swiglu):
-    p = ef_q8_product()
-    p.a, p.a_type, p.lda = _rows(a)
-    p.out, p.out_type, p.ldo = _rows(out)
-    if str(w.dtype) != "torch.int8" or w.dim() not in (2, 3) or (w.shape[-1] > 1 and w.stride(-1) != 1):
+    a_ptr, a_type, lda = _rows(a)
+    out_ptr, out_type, ldo = _rows(out)
+    shape, strides = w.shape, w.stride()
+    if len(shape) not in (2, 3) or _kinds.get(w.dtype) != EF_I8 or (shape[-1] > 1 and strides[-1] != 1):
         raise EfError(EF_EINVAL, "ef_matmul_q8: w must be int8 [N, K] or [G, N, K] with consecutive row elements")
-    p.G, (p.N, p.K) = (w.shape[0] if w.dim() == 3 else 1), w.shape[-2:]
-    p.w, p.ldw = w.data_ptr(), w.stride(-2) if p.N > 1 else (p.K + 15) // 16 * 16
-    p.w_group = w.stride(0) if p.G > 1 else 0
-    cols = p.N // 2 if swiglu else p.N
-    if a.shape[1] < p.K or (p.a_type != EF_I8 and a.shape[1] != p.K):
-        raise EfError(EF_EINVAL, f"ef_matmul_q8: rows of {a.shape[1]} against K = {p.K}")
-    p.a_rows, p.M = a.shape[0], out.shape[0]
-    if (out.shape[1] != cols or w_scale.numel() != p.G * p.N or (rows is not None and rows.numel() < p.M)
-            or (offsets is not None and offsets.numel() != p.G + 1) or (a_scale is not None and a_scale.numel() < p.a_rows)):
+    N, K = shape[-2:]
+    G = shape[0] if len(shape) == 3 else 1
+    a_rows, a_cols = a.shape
+    M, cols = out.shape
+    if a_cols < K or (a_type != EF_I8 and a_cols != K):
+        raise EfError(EF_EINVAL, f"ef_matmul_q8: rows of {a_cols} against K = {K}")
+    if (cols != (N // 2 if swiglu else N) or w_scale.numel() != G * N or (rows is not None and rows.numel() < M)
+            or (offsets is not None and offsets.numel() != G + 1) or (a_scale is not None and a_scale.numel() < a_rows)):
         raise EfError(EF_EINVAL, "ef_matmul_q8: out, scales, rows or offsets do not fit the product")
-    p.a_scale, p.rows, p.offsets, p.w_scale = _ptr(a_scale), _ptr(rows), _ptr(offsets), _ptr(w_scale)
-    p.row_div, p.swiglu = row_div, int(swiglu)
-    return p
+    return ef_q8_product(a_ptr, _ptr(a_scale), _ptr(rows), _ptr(offsets), w.data_ptr(), _ptr(w_scale), out_ptr, lda,
+                         strides[-2] if N > 1 else (K + 15) // 16 * 16, strides[0] if G > 1 else 0, ldo, a_type, out_type, a_rows, M, N, K,
+                         G, row_div, bool(swiglu))
 
 
 def ef_matmul_q8_work(a, w, w_scale, out, *, a_scale=None, rows=None, row_div=1, offsets=None, swiglu=False):

@@ -42,11 +42,12 @@ struct QuantArgs {
 };
 hipError_t launch_quant_rows(const QuantArgs &a, hipStream_t s);
 
-// `a` as codes whose rows are zero from K up to the next multiple of 64
+// `a`: codes whose rows are zero from K up to the next multiple of 64, or, where q8_product_quantises(), the caller's rows
 struct Q8Args {
     const int8_t *a;
-    long long lda;
-    const float *a_scale;
+    long long lda;         // elements from row to row
+    int a_type;            // EF_I8: codes
+    const float *a_scale;  // of codes; null otherwise
     int a_rows;
     const int32_t *rows;
     int row_div, M;
@@ -60,6 +61,7 @@ struct Q8Args {
     int out_type;
     long long ldo;
 };
+bool q8_product_quantises(const Q8Args &a);
 hipError_t launch_q8_product(const Q8Args &a, hipStream_t s);
 // ef_q8_tiled.hip: `wide` = tiles of 256 x 256, otherwise of 128 x 128
 hipError_t launch_q8_tiled(const Q8Args &a, bool wide, hipStream_t s);

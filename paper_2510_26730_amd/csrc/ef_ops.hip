@@ -140,6 +140,7 @@ extern "C" int ef_matmul_q8(const ef_q8_product *p, void *work, size_t work_byte
     ef::Q8Args q{};
     q.a = static_cast<const int8_t *>(p->a);
     q.lda = p->lda;
+    q.a_type = p->a_type;
     q.a_scale = p->a_scale;
     q.a_rows = p->a_rows;
     q.rows = p->rows;
@@ -161,13 +162,16 @@ extern "C" int ef_matmul_q8(const ef_q8_product *p, void *work, size_t work_byte
     if (!q8_in_place(p)) {
         if (!work || !aligned16(work)) return fail(nullptr, EF_EINVAL, "ef_matmul_q8: scratch is null or not 16-byte aligned");
         if (work_bytes < ef_matmul_q8_work(p)) return fail(nullptr, EF_EINVAL, "ef_matmul_q8: %zu bytes of scratch, %zu needed", work_bytes, ef_matmul_q8_work(p));
-        int8_t *codes = static_cast<int8_t *>(work);
-        float *scales = reinterpret_cast<float *>(codes + rounded((size_t)p->a_rows * q8_pitch(p->K)));
-        const ef::QuantArgs qa{p->a, p->a_type, p->lda, p->a_rows, p->K, codes, q8_pitch(p->K), scales};
-        EF_HIP(nullptr, ef::launch_quant_rows(qa, s));
-        q.a = codes;
-        q.lda = q8_pitch(p->K);
-        if (p->a_type != EF_I8) q.a_scale = scales;
+        if (!ef::q8_product_quantises(q)) {
+            int8_t *codes = static_cast<int8_t *>(work);
+            float *scales = reinterpret_cast<float *>(codes + rounded((size_t)p->a_rows * q8_pitch(p->K)));
+            const ef::QuantArgs qa{p->a, p->a_type, p->lda, p->a_rows, p->K, codes, q8_pitch(p->K), scales};
+            EF_HIP(nullptr, ef::launch_quant_rows(qa, s));
+            q.a = codes;
+            q.lda = q8_pitch(p->K);
+            q.a_type = EF_I8;
+            if (p->a_type != EF_I8) q.a_scale = scales;
+        }
     }
     EF_HIP(nullptr, ef::launch_q8_product(q, s));
     return EF_OK;

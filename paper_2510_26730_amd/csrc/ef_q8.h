@@ -94,7 +94,7 @@ __device__ __forceinline__ Q8Row q8_row(const Q8Args &p, int i) {
         r = r < 0 ? -1 : r / p.row_div;
     }
     if (r < 0 || r >= p.a_rows) return Q8Row{0, __builtin_nanf("")};
-    return Q8Row{r, p.a_scale[r]};
+    return Q8Row{r, p.a_scale ? p.a_scale[r] : 0.f};
 }
 
 template <int TYPE>

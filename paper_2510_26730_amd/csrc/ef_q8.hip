@@ -10,6 +10,8 @@
 #include "ef_ops.h"
 #include "ef_q8.h"
 
+#include <algorithm>
+
 namespace ef {
 
 namespace {
@@ -179,6 +181,59 @@ typedef int int4v __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ int4v load16(const int8_t *p) { return *reinterpret_cast<const int4v *>(p); }
 
+// Bytes from row to row of the codes in LDS: whole steps of 128, and 16 more that put neighbouring rows on different banks
+__host__ __device__ inline int q8_tile_pitch(int K) { return (K + 127) / 128 * 128 + 16; }
+
+// Quantises the n product rows from row0 on into LDS, zero from K to the end of the last step; a wave takes 64 pieces of 16 bytes of a
+// row at a time.  Returns the scale of row (lane % 16).  Rows are read twice, the second time from the caches.
+template <int NW, int TYPE>
+__device__ __forceinline__ void quant_tile_codes(const Q8Args &p, int row0, int n, int pitch, int8_t *codes, uint32_t *most) {
+    constexpr int kPer = TYPE == EF_F32 ? 4 : 8;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int per_row = ((p.K + 127) / 128 * 128 / kPer + 63) / 64, units = n * per_row;
+    const auto piece = [&](int unit, int &r, int &e) {
+        r = unit / per_row;
+        e = ((unit - r * per_row) * 64 + lane) * kPer;
+        const Q8Row src = q8_row(p, row0 + r);
+        return e < p.K ? *reinterpret_cast<const uint4 *>(reinterpret_cast<const char *>(p.a) + ((size_t)src.row * p.lda + e) * (16 / kPer))
+                       : make_uint4(0, 0, 0, 0);
+    };
+    for (int u = wave; u < units; u += NW) {
+        int r, e;
+        const uint4 v = piece(u, r, e);
+        uint32_t m = larger<TYPE>(larger<TYPE>(larger<TYPE>(larger<TYPE>(0, v.x), v.y), v.z), v.w);
+        if constexpr (TYPE != EF_F32) m = __builtin_bit_cast(uint32_t, to_float<TYPE>((uint16_t)max(m & 0xFFFFu, m >> 16)));
+        for (int off = 32; off >= 1; off >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off));
+        if (lane == 0) atomicMax(&most[r], m);
+    }
+    __syncthreads();
+    for (int u = wave; u < units; u += NW) {
+        int r, e;
+        const uint4 q = piece(u, r, e);
+        const uint32_t m = most[r];
+        const float s = fmaxf(__builtin_bit_cast(float, m) / 127.f, 0x1p-126f), inv = 1.f / s;
+        float v[kPer];
+        unpack16<TYPE>(q, v);
+        if (e < pitch - 16)
+#pragma unroll
+            for (int w = 0; w < kPer / 4; ++w)
+                reinterpret_cast<uint32_t *>(codes + r * pitch + e)[w] = m >= 0x7F800000u ? 0 : quant_four(v + 4 * w, s, inv);
+    }
+}
+template <int NW>
+__device__ __forceinline__ float quant_tile(const Q8Args &p, int row0, int n, int pitch, int8_t *codes, uint32_t *most) {
+    if (threadIdx.x < 16) most[threadIdx.x] = 0;
+    __syncthreads();
+    if (p.a_type == EF_F32) quant_tile_codes<NW, EF_F32>(p, row0, n, pitch, codes, most);
+    else if (p.a_type == EF_BF16) quant_tile_codes<NW, EF_BF16>(p, row0, n, pitch, codes, most);
+    else quant_tile_codes<NW, EF_F16>(p, row0, n, pitch, codes, most);
+    __syncthreads();
+    const int r = min((int)threadIdx.x & 15, n - 1);
+    const uint32_t m = most[r];
+    const Q8Row src = q8_row(p, row0 + r);
+    return m >= 0x7F800000u || src.scale != src.scale ? __builtin_nanf("") : fmaxf(__builtin_bit_cast(float, m) / 127.f, 0x1p-126f);
+}
+
 // A wave: NB blocks of 16 matrix rows (swiglu: 16 gate and their 16 up rows) for TT tiles of 16 product rows, in steps of 128 codes,
 // DEPTH steps in flight; K in KS parts over the waves of a workgroup, which are added in LDS.
 //
@@ -196,10 +251,15 @@ __device__ __forceinline__ void swap_halves(int4v &lo, int4v &hi, bool upper) {
     }
 }
 
-template <int TT, bool PAIR, int NB, int KS, int DEPTH>
+// QUANT: `a` is not codes yet.  The workgroup quantises its tile's rows into LDS itself, while its first weights are on their way, and
+// the launch that would have done so is saved; every workgroup repeats it, so it is for a few rows.
+template <int TT, bool PAIR, int NB, int KS, int DEPTH, bool QUANT>
 __global__ __launch_bounds__(64 * (KS > 4 ? KS : 4)) void q8_stream_kernel(Q8Args p) {
     static_assert(!PAIR || NB == 2, "gate and up");
+    static_assert(!QUANT || TT == 1, "few rows");
     constexpr int kWaves = KS > 4 ? KS : 4;
+    extern __shared__ __attribute__((aligned(16))) int8_t tile_codes[];   // QUANT: M rows of q8_tile_pitch bytes
+    __shared__ uint32_t tile_most[QUANT ? 16 : 1];
     __shared__ int4v sums[KS > 1 ? kWaves : 1][NB * TT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Q8Tile t;
@@ -236,11 +296,17 @@ __global__ __launch_bounds__(64 * (KS > 4 ? KS : 4)) void q8_stream_kernel(Q8Arg
 
     const int8_t *x[TT][2];
     float xs[TT], ws[NB][4];
+    if constexpr (QUANT) {
+        const int n = t.row_end - t.row0, pitch = q8_tile_pitch(p.K);
+        xs[0] = quant_tile<kWaves>(p, t.row0, n, pitch, tile_codes, tile_most);
+        x[0][0] = tile_codes + min(i, n - 1) * pitch + 32 * g;
+    } else {
 #pragma unroll
-    for (int j = 0; j < TT; ++j) {
+        for (int j = 0; j < TT; ++j) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) x[j][h] = p.a + (size_t)q8_row(p, min(t.row0 + 16 * j + 8 * h + (lane & 7), t.row_end - 1)).row * p.lda;
-        xs[j] = q8_row(p, min(t.row0 + 16 * j + i, t.row_end - 1)).scale;
+            for (int h = 0; h < 2; ++h) x[j][h] = p.a + (size_t)q8_row(p, min(t.row0 + 16 * j + 8 * h + (lane & 7), t.row_end - 1)).row * p.lda;
+            xs[j] = q8_row(p, min(t.row0 + 16 * j + i, t.row_end - 1)).scale;
+        }
     }
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -252,6 +318,11 @@ __global__ __launch_bounds__(64 * (KS > 4 ? KS : 4)) void q8_stream_kernel(Q8Arg
     // Rows of `a` are zero from K up to x_end, a multiple of 64; chunks behind it are read from before it and cleared
     const int x_end = (p.K + 63) & ~63;
     const auto fetch_x = [&](int u, int s) {
+        if constexpr (QUANT) {
+            xb[0][0][u] = load16(x[0][0] + min(s, s1 - 1) * 128);
+            xb[0][1][u] = load16(x[0][0] + min(s, s1 - 1) * 128 + 16);
+            return;
+        }
         const int k = min(min(s, s1 - 1) * 128 + 16 * (lane >> 3), x_end - 16);
 #pragma unroll
         for (int j = 0; j < TT; ++j)
@@ -269,11 +340,13 @@ __global__ __launch_bounds__(64 * (KS > 4 ? KS : 4)) void q8_stream_kernel(Q8Arg
         for (int u = 0; u < DEPTH; ++u) fetch_x(u, s0 + u);
         const bool upper = lane & 8;
         const auto multiply = [&](int u, int s) {
+            if constexpr (!QUANT) {
 #pragma unroll
-            for (int j = 0; j < TT; ++j) swap_halves(xb[j][0][u], xb[j][1][u], upper);
-            if (s * 128 + 128 > x_end && g >= 2) {
+                for (int j = 0; j < TT; ++j) swap_halves(xb[j][0][u], xb[j][1][u], upper);
+                if (s * 128 + 128 > x_end && g >= 2) {
 #pragma unroll
-                for (int j = 0; j < TT; ++j) xb[j][0][u] = xb[j][1][u] = int4v{0, 0, 0, 0};
+                    for (int j = 0; j < TT; ++j) xb[j][0][u] = xb[j][1][u] = int4v{0, 0, 0, 0};
+                }
             }
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
@@ -335,16 +408,21 @@ __global__ __launch_bounds__(64 * (KS > 4 ? KS : 4)) void q8_stream_kernel(Q8Arg
     }
 }
 
-template <int TT, bool PAIR>
+template <int TT, bool PAIR, bool QUANT>
 hipError_t launch_stream(const Q8Args &p, hipStream_t s) {
     const int cols = PAIR ? p.N / 2 : p.N, tiles = q8_tiles_bound(p, 16 * TT);
     const int b16 = (cols + 15) / 16, b32 = (cols + 31) / 32, wide = PAIR ? b16 : b32;   // waves per tile without a split of K
+    const size_t lds = QUANT ? (size_t)p.M * q8_tile_pitch(p.K) : 0;
     if (tiles > 65535) return hipErrorInvalidValue;
     const long long waves = (long long)wide * tiles;
-    if (waves >= 2048) hipLaunchKernelGGL((q8_stream_kernel<TT, PAIR, 2, 1, 1>), dim3((wide + 3) / 4, tiles), dim3(256), 0, s, p);
-    else if (PAIR || TT > 1 || waves >= 512) hipLaunchKernelGGL((q8_stream_kernel<TT, PAIR, 2, 4, 2>), dim3(wide, tiles), dim3(256), 0, s, p);
-    else if constexpr (!PAIR && TT == 1) hipLaunchKernelGGL((q8_stream_kernel<1, false, 1, 8, 4>), dim3(b16, tiles), dim3(512), 0, s, p);
+    if (waves >= 2048) hipLaunchKernelGGL((q8_stream_kernel<TT, PAIR, 2, 1, 1, QUANT>), dim3((wide + 3) / 4, tiles), dim3(256), lds, s, p);
+    else if (PAIR || TT > 1 || waves >= 512) hipLaunchKernelGGL((q8_stream_kernel<TT, PAIR, 2, 4, 2, QUANT>), dim3(wide, tiles), dim3(256), lds, s, p);
+    else if constexpr (!PAIR && TT == 1) hipLaunchKernelGGL((q8_stream_kernel<1, false, 1, 8, 4, QUANT>), dim3(b16, tiles), dim3(512), lds, s, p);
     return hipGetLastError();
+}
+template <int TT, bool QUANT>
+hipError_t launch_stream(const Q8Args &p, hipStream_t s) {
+    return p.swiglu ? launch_stream<TT, true, QUANT>(p, s) : launch_stream<TT, false, QUANT>(p, s);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -413,11 +491,20 @@ hipError_t launch_quant_rows(const QuantArgs &a, hipStream_t s) {
     }
 }
 
+// Whether the product quantises rows itself (p.a: the rows as they are): up to four rows, one matrix, aligned to 16 bytes, whose codes
+// fit LDS.  1 x 4096 x 4096: 7 us in one launch against 3 + 6 and the gap between two.  Not for groups, whose tiles need LDS for 16
+// rows each and run four instead of five to a compute unit: 32 tokens of 64 experts, first half, 74 against 4.6 + 64.5 us.
+bool q8_product_quantises(const Q8Args &p) {
+    const int per = p.a_type == EF_F32 ? 4 : 8;
+    return p.a_type != EF_I8 && p.G == 1 && p.M <= 4 && p.K % per == 0 && p.lda % per == 0 && reinterpret_cast<size_t>(p.a) % 16 == 0 &&
+           p.M * q8_tile_pitch(p.K) <= 64 * 1024;
+}
+
 hipError_t launch_q8_product(const Q8Args &p, hipStream_t s) {
     if (p.M <= 0) return hipSuccess;
     const int per = (p.M + p.G - 1) / p.G;
+    if (p.a_type != EF_I8) return q8_product_quantises(p) ? launch_stream<1, true>(p, s) : hipErrorInvalidValue;
     if (per > 64) return launch_q8_tiled(p, per > 512, s);
-    if (p.swiglu) return per <= 16 ? launch_stream<1, true>(p, s) : per <= 32 ? launch_stream<2, true>(p, s) : launch_stream<4, true>(p, s);
     return per <= 16 ? launch_stream<1, false>(p, s) : per <= 32 ? launch_stream<2, false>(p, s) : launch_stream<4, false>(p, s);
 }
 
