@@ -1,6 +1,7 @@
 // What the kernels of the 8-bit products share: which rows a workgroup takes, and how results leave.
 #pragma once
 #include "ef_device.h"
+#include "ef_kernels.h"
 #include "ef_ops.h"
 
 namespace ef {
@@ -71,18 +72,59 @@ __device__ __forceinline__ bool q8_find_tile(const Q8Args &p, int index, int til
     return false;
 }
 
-// tiles of `tile` rows that the groups make
-__device__ __forceinline__ int q8_total_tiles(const Q8Args &p, int tile) {
-    if (!p.offsets) return (p.M + tile - 1) / tile;
-    int total = 0, end = 0;
-    for (int g0 = 0; g0 < p.G; g0 += 64) {
-        int lo, hi;
-        q8_group_rows(p, g0, end, lo, hi);
-        int n = (hi - lo + tile - 1) / tile;
-        for (int o = 32; o >= 1; o >>= 1) n += __shfl_xor(n, o);
-        total += __builtin_amdgcn_readfirstlane(n);
+// The unit (panel of matrix rows x tile of `tile` product rows) of workgroup `block`, of `npanels` panels: an even, contiguous share
+// of all units for each XCD (workgroups go to the XCDs in turn), walked in the order of tiled_unit().  t.row0 / row_end are the
+// tile's; false for workgroups past their XCD's share.
+__device__ __forceinline__ bool q8_find_unit(const Q8Args &p, int block, int npanels, int tile, Q8Tile &t, int &panel) {
+    const int part = block & 7, local = block >> 3;
+    if (!p.offsets) {
+        t.tiles = (p.M + tile - 1) / tile;
+        t.group = t.first = t.lo = 0;
+        t.hi = p.M;
     }
-    return total;
+    int u;
+    if (p.offsets && p.G <= 64) {      // one walk
+        const int lane = threadIdx.x & 63;
+        int end = 0, lo, hi;
+        q8_group_rows(p, 0, end, lo, hi);
+        const int n = (hi - lo + tile - 1) / tile;
+        int incl = n;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(incl, o);
+            if (lane >= o) incl += v;
+        }
+        const int units = __builtin_amdgcn_readlane(incl, 63) * npanels;
+        u = tiled_xcd_begin(units, part) + local;
+        if (u >= tiled_xcd_begin(units, part + 1)) return false;
+        const int l = __builtin_ctzll(__ballot(incl > u / npanels));
+        t.group = l;
+        t.first = __builtin_amdgcn_readlane(incl - n, l);
+        t.tiles = __builtin_amdgcn_readlane(n, l);
+        t.lo = __builtin_amdgcn_readlane(lo, l);
+        t.hi = __builtin_amdgcn_readlane(hi, l);
+    } else {
+        int total = t.tiles, end = 0;
+        if (p.offsets) {
+            total = 0;
+            for (int g0 = 0; g0 < p.G; g0 += 64) {
+                int lo, hi;
+                q8_group_rows(p, g0, end, lo, hi);
+                int n = (hi - lo + tile - 1) / tile;
+                for (int o = 32; o >= 1; o >>= 1) n += __shfl_xor(n, o);
+                total += __builtin_amdgcn_readfirstlane(n);
+            }
+        }
+        const int units = total * npanels;
+        u = tiled_xcd_begin(units, part) + local;
+        if (u >= tiled_xcd_begin(units, part + 1)) return false;
+        if (p.offsets && !q8_find_tile(p, u / npanels, tile, t)) return false;
+    }
+    const TiledUnit unit = tiled_unit(u - t.first * npanels, npanels, t.tiles);
+    panel = unit.np;
+    t.row0 = t.lo + unit.mp * tile;
+    t.row_end = min(t.hi, t.row0 + tile);
+    return true;
 }
 
 // the row of `a` behind a product row, and its scale; one that does not exist reads row 0 and counts as NaN

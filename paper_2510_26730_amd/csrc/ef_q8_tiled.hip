@@ -54,20 +54,15 @@ __global__ __launch_bounds__(256, RA *RB >= 16 ? 1 : 2) void q8_tiled_kernel(Q8A
     static_assert(RA == RB, "reads alternate between the operands");
     constexpr int kSlabs = 4 * (RA + RB), kStageBytes = kSlabs * 1024, kLoads = RA + RB;
     __shared__ __attribute__((aligned(16))) char lds[kStages * kStageBytes];
+    __shared__ __attribute__((aligned(16))) float wscale[64 * RA], xscale[64 * RB];   // of the rows in the order of their slabs
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wf = wave & 1, wt = wave >> 1;
 
-    // the unit of this workgroup: an even, contiguous share of all units per XCD (workgroups go to the XCDs in turn)
-    const int units = q8_total_tiles(p, 64 * RB) * npanels, part = blockIdx.x & 7;
-    const int u = tiled_xcd_begin(units, part) + (int)(blockIdx.x >> 3);
-    if (u >= tiled_xcd_begin(units, part + 1)) return;
     Q8Tile t;
-    if (!q8_find_tile(p, u / npanels, 64 * RB, t)) return;
-    const TiledUnit unit = tiled_unit(u - t.first * npanels, npanels, t.tiles);
-    t.row0 = t.lo + unit.mp * 64 * RB;
-    t.row_end = min(t.hi, t.row0 + 64 * RB);
+    int panel;
+    if (!q8_find_unit(p, blockIdx.x, npanels, 64 * RB, t, panel)) return;
     const int F = p.N >> 1, n_end = PAIR ? F : p.N;
-    const int n0 = unit.np * (PAIR ? 32 * RA : 64 * RA);
+    const int n0 = panel * (PAIR ? 32 * RA : 64 * RA);
     const int nstage = (p.K + 63) >> 6;
 
     // this lane's rows; columns past the end and rows past the group's read a neighbour's codes, their results are dropped
@@ -111,6 +106,12 @@ __global__ __launch_bounds__(256, RA *RB >= 16 ? 1 : 2) void q8_tiled_kernel(Q8A
             for (int v = 0; v < 16; ++v) acc[x][y][v] = 0;
     int4v a0[RA], b0[RB], a1[RA], b1[RB];
 
+    // scales ahead of the first loads: what waits for them is the waits' first round at most
+    for (int r = tid; r < 64 * RA; r += 256) {
+        const int i = r & 31, ab = r >> 5;
+        wscale[r] = p.w_scale[(size_t)t.group * p.N + (PAIR ? (ab & 1) * F + min(n0 + (ab >> 1) * 32 + i, F - 1) : min(n0 + r, p.N - 1))];
+    }
+    for (int r = tid; r < 64 * RB; r += 256) xscale[r] = q8_row(p, min(t.row0 + r, t.row_end - 1)).scale;
     static_for<0, kStages - 1>([&](auto st) { static_for<0, kLoads>([&](auto q) { load(decltype(st)::value, q); }); });
     __builtin_amdgcn_s_waitcnt(wait_vm(kLoads * (kStages - 2)));   // my part of stage 0 has landed
     __syncthreads();
@@ -155,14 +156,13 @@ __global__ __launch_bounds__(256, RA *RB >= 16 ? 1 : 2) void q8_tiled_kernel(Q8A
     // share of the ring: 16 bytes per lane back, neighbouring lanes neighbouring pieces of a row.
     constexpr int kCols = PAIR ? 16 * RA : 32 * RA;        // output columns of the wave
     const int g = lane >> 5, col0 = n0 + wf * kCols;
-    const float *ws = p.w_scale + (size_t)t.group * p.N;
     float sc[RA][16];
 #pragma unroll
     for (int x = 0; x < RA; ++x)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            const int c = 8 * (v >> 2) + 4 * g + (v & 3);
-            sc[x][v] = PAIR ? ws[(x & 1) * F + min(col0 + (x >> 1) * 32 + c, F - 1)] : ws[min(col0 + x * 32 + c, p.N - 1)];
+        for (int q = 0; q < 4; ++q) {
+            const float4 f = *reinterpret_cast<const float4 *>(&wscale[(wf * RA + x) * 32 + 8 * q + 4 * g]);
+            sc[x][4 * q] = f.x, sc[x][4 * q + 1] = f.y, sc[x][4 * q + 2] = f.z, sc[x][4 * q + 3] = f.w;
         }
     const int size = p.out_type == EF_F32 ? 4 : 2, pitch = kCols * size + 16;
     char *mine = lds + wave * (kStages * kStageBytes / 4);
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(256, RA *RB >= 16 ? 1 : 2) void q8_tiled_kernel(Q8A
     for (int y = 0; y < RB; ++y) {
         const int row0 = t.row0 + (wt * RB + y) * 32;
         if (row0 >= t.row_end) break;
-        const float xs = q8_row(p, min(row0 + i, t.row_end - 1)).scale;
+        const float xs = xscale[(wt * RB + y) * 32 + i];
 #pragma unroll
         for (int x = 0; x < RA; x += PAIR ? 2 : 1)
 #pragma unroll
@@ -186,17 +186,31 @@ __global__ __launch_bounds__(256, RA *RB >= 16 ? 1 : 2) void q8_tiled_kernel(Q8A
                 q8_put4(mine + i * pitch, (PAIR ? x / 2 : x) * 32 + 8 * q + 4 * g, p.out_type, v);
             }
         wave_lds_sync();
-        const int per_row = kCols * size / 16, rows = min(32, t.row_end - row0);
-        for (int z = lane; z < 32 * per_row; z += 64) {
-            const int r = z / per_row, piece = z - r * per_row, elems = 16 / size, c = col0 + piece * elems;
-            if (r >= rows || c >= n_end) continue;
-            const char *from = mine + r * pitch + piece * 16;
-            char *to = static_cast<char *>(p.out) + ((size_t)(row0 + r) * p.ldo + c) * size;
-            if (whole && c + elems <= n_end) *reinterpret_cast<uint4 *>(to) = *reinterpret_cast<const uint4 *>(from);
-            else if (size == 4)
-                for (int e = 0; e < 4 && c + e < n_end; ++e) reinterpret_cast<float *>(to)[e] = reinterpret_cast<const float *>(from)[e];
-            else
-                for (int e = 0; e < 8 && c + e < n_end; ++e) reinterpret_cast<uint16_t *>(to)[e] = reinterpret_cast<const uint16_t *>(from)[e];
+        const int rows = min(32, t.row_end - row0);
+        char *to = static_cast<char *>(p.out) + ((size_t)row0 * p.ldo + col0) * size;
+        if (whole && col0 + kCols <= n_end) {
+            const int per_row = kCols * size / 16;        // a power of two
+            for (int z = lane; z < rows * per_row; z += 64) {
+                const int r = z / per_row, piece = z & (per_row - 1);
+                *reinterpret_cast<uint4 *>(to + (size_t)r * p.ldo * size + piece * 16) = *reinterpret_cast<const uint4 *>(mine + r * pitch + piece * 16);
+            }
+        } else {      // an element per lane: rows that start anywhere, the last columns
+            const int cols = min(kCols, n_end - col0);
+            const auto rows_of = [&](auto type) {
+                using T = decltype(type);
+                for (int r = 0; r < rows; r += 8)
+#pragma unroll
+                    for (int c = lane; c < kCols; c += 64) {
+                        T v[8];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) v[q] = reinterpret_cast<const T *>(mine + (r + q) * pitch)[c];
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            if (c < cols && r + q < rows) reinterpret_cast<T *>(to)[(size_t)(r + q) * p.ldo + c] = v[q];
+                    }
+            };
+            if (size == 4) rows_of(0.f);
+            else rows_of((uint16_t)0);
         }
         wave_lds_sync();
     }

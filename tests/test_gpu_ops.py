@@ -261,7 +261,8 @@ def check_product(gen, x, G, N, counts=None, rows=None, row_div=1, swiglu=False,
 
 
 DENSE = [(1, 64, 32), (1, 1, 1), (2, 15, 17), (1, 4096, 48), (16, 64, 64), (17, 80, 33), (33, 1000, 40), (64, 129, 100), (65, 256, 257),
-         (100, 192, 300), (128, 128, 128), (130, 2049, 130), (200, 512, 513), (257, 320, 260), (300, 64, 96), (700, 1000, 520), (1100, 448, 264)]
+         (100, 192, 300), (128, 128, 128), (130, 2049, 130), (200, 512, 513), (257, 320, 260), (300, 64, 96), (700, 1000, 520), (1100, 448, 264),
+         (4, 16000, 40), (3, 4104, 100), (2, 13000, 33)]
 
 
 @pytest.mark.parametrize("out", ["bf16", "f16", "f32"])
