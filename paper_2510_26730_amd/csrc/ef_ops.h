@@ -65,6 +65,9 @@ bool q8_product_quantises(const Q8Args &a);
 hipError_t launch_q8_product(const Q8Args &a, hipStream_t s);
 // ef_q8_tiled.hip: `wide` = tiles of 256 x 256, otherwise of 128 x 128
 hipError_t launch_q8_tiled(const Q8Args &a, bool wide, hipStream_t s);
+// ef_q8_panel.hip
+bool q8_panel_ok(const Q8Args &a);
+hipError_t launch_q8_panel(const Q8Args &a, hipStream_t s);
 
 struct CombineArgs {
     const void *y;

@@ -6,6 +6,10 @@
 
 namespace ef {
 
+typedef int int4v __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ int4v load16(const int8_t *p) { return *reinterpret_cast<const int4v *>(p); }
+
 // a tile of product rows: rows row0 .. row_end-1 of a group, which has rows lo .. hi-1, `tiles` tiles and the first one's number
 struct Q8Tile { int group, row0, row_end, lo, hi, first, tiles; };
 
@@ -137,6 +141,20 @@ __device__ __forceinline__ Q8Row q8_row(const Q8Args &p, int i) {
     }
     if (r < 0 || r >= p.a_rows) return Q8Row{0, __builtin_nanf("")};
     return Q8Row{r, p.a_scale ? p.a_scale[r] : 0.f};
+}
+
+// A load of a wave takes 8 rows x 128 bytes, whole lines: lane 8c + r gets chunk c (16 bytes) of row r, or of row 8 + r in the second
+// load.  The matrix instruction wants row i in the lanes i, i + 16, i + 32, i + 48, so the halves of 16 lanes swap: of the first load
+// the upper half (odd chunks of rows 0..7) against the lower half of the second one (even chunks of rows 8..15).  Then every lane has
+// chunks 2g and 2g + 1 of its own row.  Loads of 16 rows x 64 bytes, which need no swap, were slower: MEASURED_STREAM.
+__device__ __forceinline__ void swap_halves(int4v &lo, int4v &hi, bool upper) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int away = upper ? lo[e] : hi[e];
+        const int back = __builtin_amdgcn_mov_dpp(away, 0x128, 0xf, 0xf, true);   // 16 lanes rotated by 8
+        lo[e] = upper ? back : lo[e];
+        hi[e] = upper ? hi[e] : back;
+    }
 }
 
 template <int TYPE>

@@ -177,9 +177,6 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(QuantArgs a) {
 // ------------------------------------------------------------------------------------------------
 // products, streamed
 // ------------------------------------------------------------------------------------------------
-typedef int int4v __attribute__((ext_vector_type(4)));
-
-__device__ __forceinline__ int4v load16(const int8_t *p) { return *reinterpret_cast<const int4v *>(p); }
 
 // Bytes from row to row of the codes in LDS: whole steps of 128, and 16 more that put neighbouring rows on different banks
 __host__ __device__ inline int q8_tile_pitch(int K) { return (K + 127) / 128 * 128 + 16; }
@@ -237,20 +234,6 @@ __device__ __forceinline__ float quant_tile(const Q8Args &p, int row0, int n, in
 // A wave: NB blocks of 16 matrix rows (swiglu: 16 gate and their 16 up rows) for TT tiles of 16 product rows, in steps of 128 codes,
 // DEPTH steps in flight; K in KS parts over the waves of a workgroup, which are added in LDS.
 //
-// A load of a wave takes 8 rows x 128 bytes, whole lines: lane 8c + r gets chunk c (16 bytes) of row r, or of row 8 + r in the second
-// load.  The matrix instruction wants row i in the lanes i, i + 16, i + 32, i + 48, so the halves of 16 lanes swap: of the first load
-// the upper half (odd chunks of rows 0..7) against the lower half of the second one (even chunks of rows 8..15).  Then every lane has
-// chunks 2g and 2g + 1 of its own row.  Loads of 16 rows x 64 bytes, which need no swap, were slower: MEASURED_STREAM.
-__device__ __forceinline__ void swap_halves(int4v &lo, int4v &hi, bool upper) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int away = upper ? lo[e] : hi[e];
-        const int back = __builtin_amdgcn_mov_dpp(away, 0x128, 0xf, 0xf, true);   // 16 lanes rotated by 8
-        lo[e] = upper ? back : lo[e];
-        hi[e] = upper ? hi[e] : back;
-    }
-}
-
 // QUANT: `a` is not codes yet.  The workgroup quantises its tile's rows into LDS itself, while its first weights are on their way, and
 // the launch that would have done so is saved; every workgroup repeats it, so it is for a few rows.
 template <int TT, bool PAIR, int NB, int KS, int DEPTH, bool QUANT>
@@ -408,16 +391,28 @@ __global__ __launch_bounds__(64 * (KS > 4 ? KS : 4)) void q8_stream_kernel(Q8Arg
     }
 }
 
+// Waves that a streamed launch has without a split of K, for tiles of 16*TT rows
+long long stream_waves(const Q8Args &p, int TT) {
+    const int cols = p.swiglu ? p.N / 2 : p.N, per = p.swiglu ? 16 : 32;
+    return (long long)((cols + per - 1) / per) * q8_tiles_bound(p, 16 * TT);
+}
+
+// From 2048 waves (two per SIMD) on K stays whole; below, four waves share it; below 512, eight, with 16 columns each, so that twice
+// the workgroups share the columns (1 x 4096 x 4096 8.6 -> 7.0 us).
 template <int TT, bool PAIR, bool QUANT>
 hipError_t launch_stream(const Q8Args &p, hipStream_t s) {
     const int cols = PAIR ? p.N / 2 : p.N, tiles = q8_tiles_bound(p, 16 * TT);
-    const int b16 = (cols + 15) / 16, b32 = (cols + 31) / 32, wide = PAIR ? b16 : b32;   // waves per tile without a split of K
+    const int b16 = (cols + 15) / 16, b32 = (cols + 31) / 32, wide = PAIR ? b16 : b32;
     const size_t lds = QUANT ? (size_t)p.M * q8_tile_pitch(p.K) : 0;
     if (tiles > 65535) return hipErrorInvalidValue;
-    const long long waves = (long long)wide * tiles;
-    if (waves >= 2048) hipLaunchKernelGGL((q8_stream_kernel<TT, PAIR, 2, 1, 1, QUANT>), dim3((wide + 3) / 4, tiles), dim3(256), lds, s, p);
-    else if (PAIR || TT > 1 || waves >= 512) hipLaunchKernelGGL((q8_stream_kernel<TT, PAIR, 2, 4, 2, QUANT>), dim3(wide, tiles), dim3(256), lds, s, p);
-    else if constexpr (!PAIR && TT == 1) hipLaunchKernelGGL((q8_stream_kernel<1, false, 1, 8, 4, QUANT>), dim3(b16, tiles), dim3(512), lds, s, p);
+    const long long waves = stream_waves(p, TT);
+    if (TT < 4 && waves >= 2048) {
+        if constexpr (TT < 4) hipLaunchKernelGGL((q8_stream_kernel<TT, PAIR, 2, 1, 1, QUANT>), dim3((wide + 3) / 4, tiles), dim3(256), lds, s, p);
+    } else if (PAIR || TT > 1 || waves >= 512) {
+        hipLaunchKernelGGL((q8_stream_kernel<TT, PAIR, 2, 4, 2, QUANT>), dim3(wide, tiles), dim3(256), lds, s, p);
+    } else if constexpr (!PAIR && TT == 1) {
+        hipLaunchKernelGGL((q8_stream_kernel<1, false, 1, 8, 4, QUANT>), dim3(b16, tiles), dim3(512), lds, s, p);
+    }
     return hipGetLastError();
 }
 template <int TT, bool QUANT>
@@ -428,31 +423,62 @@ hipError_t launch_stream(const Q8Args &p, hipStream_t s) {
 // ------------------------------------------------------------------------------------------------
 // weighted sum of the expert rows of a token
 // ------------------------------------------------------------------------------------------------
-template <int YT, int OT>
+// A lane takes W columns (16 bytes of y), the rows of up to four slots in flight; sums in the order of the slots.  Bound by reading y:
+// MEASURED_COMBINE.
+template <int YT, int OT, int W>
 __global__ __launch_bounds__(256) void combine_rows_kernel(CombineArgs a) {
     using Y = typename Element<YT>::T;
     const Y *y = static_cast<const Y *>(a.y);
-    const int t = blockIdx.x;
-    for (int i = blockIdx.y * 256 + threadIdx.x; i < a.d; i += gridDim.y * 256) {
-        float sum = 0.f;
-        for (int j = 0; j < a.k; ++j) {
-            const long long slot = (long long)t * a.k + j, r = a.inv_perm ? a.inv_perm[slot] : slot;
-            const float v = r >= 0 && r < a.y_rows ? to_float<YT>(y[r * a.ldy + i]) : __builtin_nanf("");
-            sum = __builtin_fmaf(a.w[slot], v, sum);
+    const int t = blockIdx.x, c = (blockIdx.y * 256 + threadIdx.x) * W;
+    if (c >= a.d) return;
+    float sum[W];
+#pragma unroll
+    for (int e = 0; e < W; ++e) sum[e] = 0.f;
+    const long long slot0 = (long long)t * a.k;
+    for (int j0 = 0; j0 < a.k; j0 += 4) {
+        Y v[4][W];
+        float w[4];
+        bool live[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const long long slot = slot0 + min(j0 + q, a.k - 1);
+            long long r = a.inv_perm ? a.inv_perm[slot] : slot;
+            live[q] = r >= 0 && r < a.y_rows;
+            if (!live[q]) r = 0;
+            w[q] = a.w[slot];
+            if constexpr (W > 1) *reinterpret_cast<uint4 *>(v[q]) = *reinterpret_cast<const uint4 *>(y + r * a.ldy + c);
+            else v[q][0] = y[r * a.ldy + c];
         }
-        store_element<OT>(a.out, (size_t)t * a.ldo + i, sum);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (j0 + q < a.k)
+#pragma unroll
+                for (int e = 0; e < W; ++e) sum[e] = __builtin_fmaf(w[q], live[q] ? to_float<YT>(v[q][e]) : __builtin_nanf(""), sum[e]);
+    }
+    const size_t at = (size_t)t * a.ldo + c;
+    if constexpr (W == 1) store_element<OT>(a.out, at, sum[0]);
+    else {
+#pragma unroll
+        for (int e = 0; e < W; e += 4) {
+            const float f[4] = {sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
+            q8_put4(static_cast<char *>(a.out) + (at + e) * (OT == EF_F32 ? 4 : 2), 0, OT, f);
+        }
     }
 }
 
+template <int YT, int OT>
+hipError_t launch_combine_rows(const CombineArgs &a, hipStream_t s) {
+    constexpr int W = YT == EF_F32 ? 4 : 8, out = OT == EF_F32 ? 4 : 2;
+    const bool whole = a.d % W == 0 && a.ldy % W == 0 && reinterpret_cast<size_t>(a.y) % 16 == 0 && a.ldo % 4 == 0 &&
+                       reinterpret_cast<size_t>(a.out) % (4 * out) == 0;
+    if (whole) hipLaunchKernelGGL((combine_rows_kernel<YT, OT, W>), dim3(a.T, (a.d / W + 255) / 256), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((combine_rows_kernel<YT, OT, 1>), dim3(a.T, (a.d + 255) / 256), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
 template <int YT>
 hipError_t launch_combine_y(const CombineArgs &a, hipStream_t s) {
-    const dim3 grid(a.T, (a.d + 255) / 256);
-    switch (a.out_type) {
-        case EF_BF16: hipLaunchKernelGGL((combine_rows_kernel<YT, EF_BF16>), grid, dim3(256), 0, s, a); break;
-        case EF_F16: hipLaunchKernelGGL((combine_rows_kernel<YT, EF_F16>), grid, dim3(256), 0, s, a); break;
-        default: hipLaunchKernelGGL((combine_rows_kernel<YT, EF_F32>), grid, dim3(256), 0, s, a); break;
-    }
-    return hipGetLastError();
+    return a.out_type == EF_BF16 ? launch_combine_rows<YT, EF_BF16>(a, s) : a.out_type == EF_F16 ? launch_combine_rows<YT, EF_F16>(a, s)
+                                                                                                 : launch_combine_rows<YT, EF_F32>(a, s);
 }
 
 }  // namespace
@@ -500,12 +526,36 @@ bool q8_product_quantises(const Q8Args &p) {
            p.M * q8_tile_pitch(p.K) <= 64 * 1024;
 }
 
+// Which form a product takes, by its sizes alone (the groups' own sizes are on the device).  Measured with codes in place; us of the
+// form taken / the next best:
+//   streamed   one matrix whose tiles of 16, 32 or 64 rows make one round of workgroups: 64 x 4096 x 4096 10.7 / 17.9 (128 x 128 tiles),
+//              128 x 4096 x 4096 15.4 / 18.7, and up to 32 rows of any width: 24 x 4096 x 14336 18.7 / 24.0 (panels); past a round,
+//              192 x 4096 x 4096, 24.6 against 18.4.  Groups of few rows where K is short, because a panel takes longer to start: 256
+//              groups of 4, 1024 x 512, 28.0 / 35.4; 64 of 3, 2048 x 2816, 64.5 / 67.0, but 64 of 8 75.9 against 71.9 and 128 of 2,
+//              4096 x 1024, 115.8 against 102.8.  Few groups at work, as with one token: 2 of 8, 14336 x 4096, 23.8 / 63.2.
+//   panels     groups of up to 40 rows: 8 of 12, 4096 x 28672, 158.9 / 171.9; 64 of 48, 1408 x 2048, 45.3 against 37.5.  One matrix and a
+//              round of panels, of up to 128 rows (4096 x 14336 25.8 / 29.6; 192 rows 41.3 against 28.8) or with rows that are not
+//              aligned to 64 bytes (512 x 5640 x 2049 31.4 / 36.6; aligned 512 x 4096 x 4096 23.3 against 20.6).
+//   256 x 256  where rows per group times K make up for the start and end of a tile, and tiles fill half of the chip and more:
+//              64 groups of 384, 2048 x 2816, 223 / 233, of 192 145 against 142; 64 of 384, 1408 x 2048, 148 against 136; 768 x 4096 x
+//              14336 (168 tiles) 58.4 / 72.5, 512 (112) 55.2 against 48.2.
+//   128 x 128  the rest.
 hipError_t launch_q8_product(const Q8Args &p, hipStream_t s) {
     if (p.M <= 0) return hipSuccess;
-    const int per = (p.M + p.G - 1) / p.G;
+    const int per = (p.M + p.G - 1) / p.G, cols = p.swiglu ? p.N / 2 : p.N;
     if (p.a_type != EF_I8) return q8_product_quantises(p) ? launch_stream<1, true>(p, s) : hipErrorInvalidValue;
-    if (per > 64) return launch_q8_tiled(p, per > 512, s);
-    return per <= 16 ? launch_stream<1, false>(p, s) : per <= 32 ? launch_stream<2, false>(p, s) : launch_stream<4, false>(p, s);
+    const auto panels = [&](int width) { return (long long)((cols + width - 1) / width); };
+    if (p.G == 1) {
+        if (p.M <= 16) return launch_stream<1, false>(p, s);
+        if (p.M <= 32 || stream_waves(p, 2) <= 256) return launch_stream<2, false>(p, s);
+        if (stream_waves(p, 4) <= 256) return launch_stream<4, false>(p, s);
+        if (q8_panel_ok(p) && (p.M <= 128 || p.ldw % 64 != 0) && panels(p.swiglu ? 64 : 128) * q8_tiles_bound(p, 64) <= 256) return launch_q8_panel(p, s);
+    } else {
+        if (per <= (p.K <= 1024 ? 16 : p.K <= 2048 ? 4 : 0) || (per <= 16 && stream_waves(p, 1) <= 2048)) return launch_stream<1, false>(p, s);
+        if (q8_panel_ok(p) && per <= 40) return launch_q8_panel(p, s);
+    }
+    const long long tiles = std::max((p.M + 255) / 256, std::min(p.G, p.M));
+    return launch_q8_tiled(p, (long long)per * p.K >= 512 * 1024 && tiles * panels(p.swiglu ? 128 : 256) >= 160, s);
 }
 
 hipError_t launch_combine_rows(const CombineArgs &a, hipStream_t s) {

@@ -1,0 +1,176 @@
+// Products of 8-bit codes, panels: one tile of 64 product rows x 128 matrix rows per workgroup, for products whose larger tiles would
+// leave compute units idle; bound by the time from a request to its data.
+//
+// Four waves share the 64 product rows and have 32 matrix rows each (swiglu: 16 gate, 16 up), in steps of 128 codes.  A weight is
+// needed by one wave only, so it goes from memory straight into that wave's operand registers; the tokens are needed by all four and
+// come through LDS by direct loads; both are requested D steps ahead.  What it measured: MEASURED_PANEL.  Up to four teams of four waves that
+// split K in a workgroup gained nothing (28.2, 28.4, 28.2, 29.6 us for 517 x 5640 x 2049): a compute unit takes in about 20 bytes a
+// clock either way.
+// A slab of 1 KiB of LDS is 8 rows x 128 codes; lane 8r + p of a load fetches chunk p ^ r, so that 16 rows at one chunk are read from
+// all banks evenly.
+#include "ef_device.h"
+#include "ef_kernels.h"
+#include "ef_ops.h"
+#include "ef_q8.h"
+
+#include <type_traits>
+
+namespace ef {
+
+namespace {
+
+constexpr int RA = 2, RB = 4;        // blocks of 16 matrix rows of a wave, of 16 product rows
+constexpr int D = 3;                 // steps on their way
+
+template <bool PAIR>
+__global__ __launch_bounds__(256) void q8_panel_kernel(Q8Args p, int npanels) {
+    constexpr int kStage = RB * 2048, kBuffers = D + 1, kLoads = RB / 2 + 2 * RA;   // loads of a step and wave
+    __shared__ __attribute__((aligned(16))) char lds[kBuffers * kStage];
+    __shared__ __attribute__((aligned(16))) float wscale[64 * RA], xscale[16 * RB];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    Q8Tile t;
+    int panel;
+    if (!q8_find_unit(p, blockIdx.x, npanels, 16 * RB, t, panel)) return;
+    const int F = p.N >> 1, n_end = PAIR ? F : p.N;
+    const int n0 = panel * (PAIR ? 32 * RA : 64 * RA), col0 = n0 + wave * (PAIR ? 8 * RA : 16 * RA);
+    const int i = lane & 15, g = lane >> 4;
+    const int steps = (p.K + 127) >> 7;
+    // matrix row behind row r (0..15) of the wave's block b; columns past the end read a neighbour's codes, their results are dropped
+    const auto matrix_row = [&](int first, int b, int r) {
+        if constexpr (PAIR) return (b < RA / 2 ? 0 : F) + min(first + (b % (RA / 2)) * 16 + r, F - 1);
+        else return min(first + b * 16 + r, p.N - 1);
+    };
+
+    const int8_t *w = p.w + (size_t)t.group * p.w_group;
+    unsigned woff[RA][2];
+#pragma unroll
+    for (int b = 0; b < RA; ++b)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) woff[b][h] = (unsigned)matrix_row(col0, b, 8 * h + (lane & 7)) * (unsigned)p.ldw;
+    const int k_last = ((p.K + 15) & ~15) - 16, x_last = ((p.K + 63) & ~63) - 16;
+    int4v wb[D][RA][2];
+    const auto fetch_w = [&](int u, int s) {
+        const unsigned k = min(min(s, steps - 1) * 128 + 16 * (lane >> 3), k_last);
+#pragma unroll
+        for (int b = 0; b < RA; ++b)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) wb[u][b][h] = load16(w + (woff[b][h] + k));
+    };
+
+    const int8_t *xsrc[RB / 2];
+#pragma unroll
+    for (int q = 0; q < RB / 2; ++q) xsrc[q] = p.a + (size_t)q8_row(p, min(t.row0 + (q * 4 + wave) * 8 + (lane >> 3), t.row_end - 1)).row * p.lda;
+    const unsigned lds_base = (unsigned)(size_t)&lds[0];
+    const int xchunk = ((lane & 7) ^ (lane >> 3)) * 16;
+    const auto load_x = [&](int buf, int s) {
+#pragma unroll
+        for (int q = 0; q < RB / 2; ++q) {
+            const int8_t *from = xsrc[q] + min(min(s, steps - 1) * 128 + xchunk, x_last);
+            const unsigned to = __builtin_amdgcn_readfirstlane(lds_base + buf * kStage + (q * 4 + wave) * 1024);
+            asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
+        }
+    };
+    // in the order of the loop, whose waits count on it
+#pragma unroll
+    for (int u = 0; u < D; ++u) {
+        load_x(u, u);
+        __builtin_amdgcn_sched_barrier(0);
+        fetch_w(u, u);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    for (int r = tid; r < 64 * RA; r += 256)
+        wscale[r] = p.w_scale[(size_t)t.group * p.N + matrix_row(n0 + (r / (16 * RA)) * (PAIR ? 8 * RA : 16 * RA), (r / 16) % RA, r & 15)];
+    for (int r = tid; r < 16 * RB; r += 256) xscale[r] = q8_row(p, min(t.row0 + r, t.row_end - 1)).scale;
+
+    int4v acc[RA][RB];
+#pragma unroll
+    for (int b = 0; b < RA; ++b)
+#pragma unroll
+        for (int j = 0; j < RB; ++j) acc[b][j] = int4v{0, 0, 0, 0};
+    const int slab = (i >> 3) * 1024 + (i & 7) * 128;
+    const int at[2] = {slab + (((2 * g) ^ (i & 7)) << 4), slab + (((2 * g + 1) ^ (i & 7)) << 4)};
+    const bool upper = lane & 8;
+    // the products of step s, weights in wb[u], tokens in LDS buffer `buf`
+    const auto multiply = [&](int u, int buf, int s) {
+#pragma unroll
+        for (int b = 0; b < RA; ++b) {
+            swap_halves(wb[u][b][0], wb[u][b][1], upper);
+            if (s * 128 + 128 > x_last + 16 && g >= 2) wb[u][b][0] = wb[u][b][1] = int4v{0, 0, 0, 0};   // past the tokens' end
+        }
+        const char *from = lds + buf * kStage;
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            int4v x[RB];
+#pragma unroll
+            for (int j = 0; j < RB; ++j) x[j] = *reinterpret_cast<const int4v *>(from + j * 2048 + at[y]);
+#pragma unroll
+            for (int j = 0; j < RB; ++j)
+#pragma unroll
+                for (int b = 0; b < RA; ++b) acc[b][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wb[u][b][y], x[j], acc[b][j], 0, 0, 0);
+        }
+    };
+    // Step s waits for its own tokens alone: its weights, and tokens and weights of the D - 1 steps behind it, may be on their way.  The
+    // compiler waits for the weights; it does not know of the loads into LDS between them, so it waits for somewhat more than it
+    // needs to.  Requests past the end repeat the last step; what is left then runs without requests.
+    int s = 0, buf = 0;
+    const auto next = [&](int b) { return b + 1 == kBuffers ? 0 : b + 1; };
+    for (; s + D < steps; s += D) {
+#pragma unroll
+        for (int u = 0; u < D; ++u) {
+            constexpr int behind = 2 * RA + (D - 1) * kLoads;
+            static_assert(behind < 64, "vmcnt is a 6-bit counter");
+            __builtin_amdgcn_s_waitcnt((behind >> 4) << 14 | 0x0F70 | (behind & 15));
+            __syncthreads();            // everybody's part has landed, and nobody reads the buffer of step s + u - 1 any more
+            load_x(buf == 0 ? kBuffers - 1 : buf - 1, s + u + D);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(u, buf, s + u);
+            __builtin_amdgcn_sched_barrier(0);
+            fetch_w(u, s + u + D);
+            __builtin_amdgcn_sched_barrier(0);
+            buf = next(buf);
+        }
+    }
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < D; ++u) {
+        if (s + u < steps) multiply(u, buf, s + u);
+        buf = next(buf);
+    }
+
+    // lane 16g + i holds product row i of its tile, matrix rows 4g .. 4g+3 of each block
+    const float *sc = wscale + wave * 16 * RA + 4 * g;
+#pragma unroll
+    for (int j = 0; j < RB; ++j) {
+        const int row = t.row0 + 16 * j + i;
+        const float xs = xscale[16 * j + i];
+        if (row >= t.row_end) continue;
+#pragma unroll
+        for (int b = 0; b < (PAIR ? RA / 2 : RA); ++b) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] = (float)acc[b][j][e] * xs * sc[16 * b + e];
+                if constexpr (PAIR) v[e] = silu_mul(v[e], (float)acc[b + RA / 2][j][e] * xs * sc[16 * (b + RA / 2) + e]);
+            }
+            q8_store4(p, row, col0 + 16 * b + 4 * g, n_end, v);
+        }
+    }
+}
+
+template <bool PAIR>
+hipError_t launch(const Q8Args &p, hipStream_t s) {
+    const int cols = PAIR ? p.N / 2 : p.N, per = PAIR ? 32 * RA : 64 * RA, npanels = (cols + per - 1) / per;
+    const long long units = (long long)q8_tiles_bound(p, 16 * RB) * npanels;
+    if (units > 0x7FFFFFF0ll || !q8_panel_ok(p)) return hipErrorInvalidValue;
+    hipLaunchKernelGGL((q8_panel_kernel<PAIR>), dim3((unsigned)((units + 7) / 8 * 8)), dim3(256), 0, s, p, npanels);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+bool q8_panel_ok(const Q8Args &p) { return (long long)p.N * p.ldw < 0x7FFFFFFFll; }      // offsets within a matrix in 32 bits
+
+hipError_t launch_q8_panel(const Q8Args &p, hipStream_t s) { return p.swiglu ? launch<true>(p, s) : launch<false>(p, s); }
+
+}  // namespace ef

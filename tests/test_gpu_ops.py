@@ -299,6 +299,33 @@ def test_product_of_groups(G, counts, K, N, swiglu):
     check_product(gen, torch.randn(T, K, generator=gen).bfloat16(), G, N, counts, rows, k, swiglu, "f32", pad_o=5, magnitude=4 / K ** 0.5)
 
 
+FORMS = [
+    # kernel, M, K, N, counts, swiglu, pitch: every form that a product can take, by the sizes that choose it
+    ("q8_stream_kernel<1, false, 1, 8", 16, 256, 256, None, False, None), ("q8_stream_kernel<1, false, 2, 4", 5, 128, 20000, None, False, None),
+    ("q8_stream_kernel<1, false, 2, 1", 7, 128, 66000, None, False, None), ("q8_stream_kernel<1, true, 2, 4", 9, 192, 512, None, True, None),
+    ("q8_stream_kernel<1, true, 2, 1", 6, 64, 66000, None, True, None), ("q8_stream_kernel<2, false, 2, 4", 30, 320, 512, None, False, None),
+    ("q8_stream_kernel<2, false, 2, 1", 18, 64, 66000, None, False, None), ("q8_stream_kernel<2, true, 2, 4", 33, 128, 320, None, True, None),
+    ("q8_stream_kernel<2, true, 2, 1", 20, 64, 66000, None, True, None), ("q8_stream_kernel<4, false, 2, 4", 200, 192, 2048, None, False, None),
+    ("q8_stream_kernel<4, true, 2, 4", 250, 64, 2000, None, True, None), ("q8_panel_kernel<false", 100, 448, 8192, None, False, None),
+    ("q8_panel_kernel<true", 70, 192, 9000, None, True, None), ("q8_panel_kernel<false", 300, 100, 5000, None, False, 112),
+    ("q8_panel_kernel<false", 0, 2560, 1024, [10] * 64 + [0, 130], False, None), ("q8_panel_kernel<true", 0, 1088, 1408, [30, 0, 1, 64, 65, 7] * 9, True, None),
+    ("q8_tiled_kernel<2, 2, false", 520, 192, 1700, None, False, None), ("q8_tiled_kernel<2, 2, true", 0, 320, 512, [90, 0, 129, 33], True, None),
+    ("q8_tiled_kernel<4, 4, false", 520, 1152, 14000, None, False, None), ("q8_tiled_kernel<4, 4, true", 0, 2112, 14000, [520, 3, 257], True, None),
+    ("q8_tiled_kernel<4, 4, false", 0, 2050, 10300, [300, 100, 385], False, 2064),
+]
+
+
+@pytest.mark.parametrize("form,M,K,N,counts,swiglu,pitch", FORMS, ids=[f"{i}-{f[0][3:].replace(' ', '')}" for i, f in enumerate(FORMS)])
+def test_every_form_of_the_product(form, M, K, N, counts, swiglu, pitch):
+    gen = torch.Generator().manual_seed(K + N)
+    M = sum(counts) if counts else M
+    x = torch.randn(M, K, generator=gen).bfloat16()
+    with torch.profiler.profile(activities=[torch.profiler.ProfilerActivity.CUDA]) as prof:
+        check_product(gen, x, len(counts) if counts else 1, N, counts, None, 1, swiglu, "bf16", pad_o=2, pitch=pitch, magnitude=4 / K ** 0.5)
+    ran = [e.name for e in prof.events() if "q8_" in e.name and "kernel" in e.name]
+    assert len(ran) == 1 and form in ran[0], ran
+
+
 @pytest.mark.parametrize("M,K,N", [(3, 64, 32), (20, 100, 40), (150, 1001, 96), (300, 128, 256), (300, 72, 128)])
 def test_product_of_codes(M, K, N):
     """Codes and scales from the caller: used in place, or padded first where whole steps cannot be read; what lies behind K is not used."""
