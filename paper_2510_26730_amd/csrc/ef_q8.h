@@ -4,6 +4,8 @@
 #include "ef_kernels.h"
 #include "ef_ops.h"
 
+#include <type_traits>
+
 namespace ef {
 
 typedef int int4v __attribute__((ext_vector_type(4)));
@@ -164,10 +166,11 @@ __device__ __forceinline__ void store_element(void *out, size_t at, float v) {
     else static_cast<__bf16 *>(out)[at] = (__bf16)v;
 }
 
-// four results, as the output type, into columns c .. c+3 of a row in LDS
-__device__ __forceinline__ void q8_put4(char *row, int c, int type, const float (&v)[4]) {
-    if (type == EF_F32) *reinterpret_cast<float4 *>(row + c * 4) = make_float4(v[0], v[1], v[2], v[3]);
-    else if (type == EF_F16) {
+// four results, as the output type, into columns c .. c+3 of a row
+template <int TYPE>
+__device__ __forceinline__ void q8_put4(char *row, int c, const float (&v)[4]) {
+    if constexpr (TYPE == EF_F32) *reinterpret_cast<float4 *>(row + c * 4) = make_float4(v[0], v[1], v[2], v[3]);
+    else if constexpr (TYPE == EF_F16) {
         typedef _Float16 h4 __attribute__((ext_vector_type(4)));
         *reinterpret_cast<h4 *>(row + c * 2) = h4{(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
     } else {
@@ -177,21 +180,26 @@ __device__ __forceinline__ void q8_put4(char *row, int c, int type, const float 
 }
 
 // columns n .. n+3 of an output row, as far as they are below n_end: one store where the four are there and aligned
+template <int TYPE>
 __device__ __forceinline__ void q8_store4(const Q8Args &p, int row, int n, int n_end, const float (&v)[4]) {
+    constexpr int size = TYPE == EF_F32 ? 4 : 2;
     const size_t at = (size_t)row * p.ldo + n;
-    const int size = p.out_type == EF_F32 ? 4 : 2;
     char *to = static_cast<char *>(p.out) + at * size;
     if (n + 4 <= n_end && (reinterpret_cast<size_t>(to) & (4 * size - 1)) == 0) {
-        q8_put4(to, 0, p.out_type, v);
+        q8_put4<TYPE>(to, 0, v);
         return;
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if (n + e >= n_end) return;
-        if (p.out_type == EF_F32) store_element<EF_F32>(p.out, at + e, v[e]);
-        else if (p.out_type == EF_F16) store_element<EF_F16>(p.out, at + e, v[e]);
-        else store_element<EF_BF16>(p.out, at + e, v[e]);
-    }
+    for (int e = 0; e < 4; ++e)
+        if (n + e < n_end) store_element<TYPE>(p.out, at + e, v[e]);
+}
+
+// calls f with the output type as a constant
+template <class F>
+__device__ __forceinline__ void q8_by_type(int type, F &&f) {
+    if (type == EF_F32) f(std::integral_constant<int, EF_F32>{});
+    else if (type == EF_F16) f(std::integral_constant<int, EF_F16>{});
+    else f(std::integral_constant<int, EF_BF16>{});
 }
 
 }  // namespace ef

@@ -371,24 +371,24 @@ __global__ __launch_bounds__(64 * (KS > 4 ? KS : 4)) void q8_stream_kernel(Q8Arg
     }
     if (n0 >= n_end) return;
     // lane 16g + i holds product row i, matrix rows 4g .. 4g+3 of each 16
+    q8_by_type(p.out_type, [&](auto TYPE) {
 #pragma unroll
-    for (int j = 0; j < TT; ++j) {
-        const int row = t.row0 + 16 * j + i;
-        if (row >= t.row_end) continue;
-        float v[NB][4];
+        for (int j = 0; j < TT; ++j) {
+            const int row = t.row0 + 16 * j + i;
+            if (row >= t.row_end) continue;
+            float v[NB][4];
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[b][e] = (float)acc[b][j][e] * xs[j] * ws[b][e];
-        if constexpr (PAIR) {
+                for (int e = 0; e < 4; ++e) v[b][e] = (float)acc[b][j][e] * xs[j] * ws[b][e];
+            if constexpr (PAIR) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[0][e] = silu_mul(v[0][e], v[1][e]);
-            q8_store4(p, row, n0 + 4 * g, n_end, v[0]);
-        } else {
+                for (int e = 0; e < 4; ++e) v[0][e] = silu_mul(v[0][e], v[1][e]);
+            }
 #pragma unroll
-            for (int b = 0; b < NB; ++b) q8_store4(p, row, n0 + 16 * b + 4 * g, n_end, v[b]);
+            for (int b = 0; b < (PAIR ? 1 : NB); ++b) q8_store4<decltype(TYPE)::value>(p, row, n0 + 16 * b + 4 * g, n_end, v[b]);
         }
-    }
+    });
 }
 
 // Waves that a streamed launch has without a split of K, for tiles of 16*TT rows
@@ -461,7 +461,7 @@ __global__ __launch_bounds__(256) void combine_rows_kernel(CombineArgs a) {
 #pragma unroll
         for (int e = 0; e < W; e += 4) {
             const float f[4] = {sum[e], sum[e + 1], sum[e + 2], sum[e + 3]};
-            q8_put4(static_cast<char *>(a.out) + (at + e) * (OT == EF_F32 ? 4 : 2), 0, OT, f);
+            q8_put4<OT>(static_cast<char *>(a.out) + (at + e) * (OT == EF_F32 ? 4 : 2), 0, f);
         }
     }
 }

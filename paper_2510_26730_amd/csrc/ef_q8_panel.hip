@@ -13,8 +13,6 @@
 #include "ef_ops.h"
 #include "ef_q8.h"
 
-#include <type_traits>
-
 namespace ef {
 
 namespace {
@@ -140,22 +138,24 @@ __global__ __launch_bounds__(256) void q8_panel_kernel(Q8Args p, int npanels) {
 
     // lane 16g + i holds product row i of its tile, matrix rows 4g .. 4g+3 of each block
     const float *sc = wscale + wave * 16 * RA + 4 * g;
+    q8_by_type(p.out_type, [&](auto TYPE) {
 #pragma unroll
-    for (int j = 0; j < RB; ++j) {
-        const int row = t.row0 + 16 * j + i;
-        const float xs = xscale[16 * j + i];
-        if (row >= t.row_end) continue;
+        for (int j = 0; j < RB; ++j) {
+            const int row = t.row0 + 16 * j + i;
+            const float xs = xscale[16 * j + i];
+            if (row >= t.row_end) continue;
 #pragma unroll
-        for (int b = 0; b < (PAIR ? RA / 2 : RA); ++b) {
-            float v[4];
+            for (int b = 0; b < (PAIR ? RA / 2 : RA); ++b) {
+                float v[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[e] = (float)acc[b][j][e] * xs * sc[16 * b + e];
-                if constexpr (PAIR) v[e] = silu_mul(v[e], (float)acc[b + RA / 2][j][e] * xs * sc[16 * (b + RA / 2) + e]);
+                for (int e = 0; e < 4; ++e) {
+                    v[e] = (float)acc[b][j][e] * xs * sc[16 * b + e];
+                    if constexpr (PAIR) v[e] = silu_mul(v[e], (float)acc[b + RA / 2][j][e] * xs * sc[16 * (b + RA / 2) + e]);
+                }
+                q8_store4<decltype(TYPE)::value>(p, row, col0 + 16 * b + 4 * g, n_end, v);
             }
-            q8_store4(p, row, col0 + 16 * b + 4 * g, n_end, v);
         }
-    }
+    });
 }
 
 template <bool PAIR>

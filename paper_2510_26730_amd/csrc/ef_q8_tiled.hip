@@ -164,40 +164,46 @@ __global__ __launch_bounds__(256, RA *RB >= 16 ? 1 : 2) void q8_tiled_kernel(Q8A
             const float4 f = *reinterpret_cast<const float4 *>(&wscale[(wf * RA + x) * 32 + 8 * q + 4 * g]);
             sc[x][4 * q] = f.x, sc[x][4 * q + 1] = f.y, sc[x][4 * q + 2] = f.z, sc[x][4 * q + 3] = f.w;
         }
-    const int size = p.out_type == EF_F32 ? 4 : 2, pitch = kCols * size + 16;
     char *mine = lds + wave * (kStages * kStageBytes / 4);
     static_assert(32 * (kCols * 4 + 16) <= kStages * kStageBytes / 4, "a tile of results fits a wave's share of the ring");
-    const bool whole = ((reinterpret_cast<size_t>(p.out) | (size_t)p.ldo * size) & 15) == 0 && (col0 * size & 15) == 0;
+    const auto leave = [&](auto TYPE) {
+        constexpr int type = decltype(TYPE)::value, size = type == EF_F32 ? 4 : 2, pitch = kCols * size + 16;
+        constexpr int kPieces = kCols * size / 16, kTurns = 32 * kPieces / 64;    // 16-byte pieces of a row; of a tile, for each lane
+        const bool whole = ((reinterpret_cast<size_t>(p.out) | (size_t)p.ldo * size) & 15) == 0 && (col0 * size & 15) == 0 && col0 + kCols <= n_end;
 #pragma unroll
-    for (int y = 0; y < RB; ++y) {
-        const int row0 = t.row0 + (wt * RB + y) * 32;
-        if (row0 >= t.row_end) break;
-        const float xs = xscale[(wt * RB + y) * 32 + i];
+        for (int y = 0; y < RB; ++y) {
+            const int row0 = t.row0 + (wt * RB + y) * 32;
+            if (row0 >= t.row_end) break;
+            const float xs = xscale[(wt * RB + y) * 32 + i];
 #pragma unroll
-        for (int x = 0; x < RA; x += PAIR ? 2 : 1)
+            for (int x = 0; x < RA; x += PAIR ? 2 : 1)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                float v[4];
+                for (int q = 0; q < 4; ++q) {
+                    float v[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    v[e] = (float)acc[x][y][4 * q + e] * xs * sc[x][4 * q + e];
-                    if constexpr (PAIR) v[e] = silu_mul(v[e], (float)acc[x + 1][y][4 * q + e] * xs * sc[x + 1][4 * q + e]);
+                    for (int e = 0; e < 4; ++e) {
+                        v[e] = (float)acc[x][y][4 * q + e] * xs * sc[x][4 * q + e];
+                        if constexpr (PAIR) v[e] = silu_mul(v[e], (float)acc[x + 1][y][4 * q + e] * xs * sc[x + 1][4 * q + e]);
+                    }
+                    q8_put4<type>(mine + i * pitch, (PAIR ? x / 2 : x) * 32 + 8 * q + 4 * g, v);
                 }
-                q8_put4(mine + i * pitch, (PAIR ? x / 2 : x) * 32 + 8 * q + 4 * g, p.out_type, v);
-            }
-        wave_lds_sync();
-        const int rows = min(32, t.row_end - row0);
-        char *to = static_cast<char *>(p.out) + ((size_t)row0 * p.ldo + col0) * size;
-        if (whole && col0 + kCols <= n_end) {
-            const int per_row = kCols * size / 16;        // a power of two
-            for (int z = lane; z < rows * per_row; z += 64) {
-                const int r = z / per_row, piece = z & (per_row - 1);
-                *reinterpret_cast<uint4 *>(to + (size_t)r * p.ldo * size + piece * 16) = *reinterpret_cast<const uint4 *>(mine + r * pitch + piece * 16);
-            }
-        } else {      // an element per lane: rows that start anywhere, the last columns
-            const int cols = min(kCols, n_end - col0);
-            const auto rows_of = [&](auto type) {
-                using T = decltype(type);
+            wave_lds_sync();
+            const int rows = min(32, t.row_end - row0);
+            char *to = static_cast<char *>(p.out) + ((size_t)row0 * p.ldo + col0) * size;
+            if (whole) {
+                const int r0 = lane / kPieces, piece = (lane & (kPieces - 1)) * 16;
+                const char *from = mine + r0 * pitch + piece;
+                to += (size_t)r0 * p.ldo * size + piece;
+                const size_t hop = (size_t)p.ldo * (size * 64 / kPieces);      // 64 / kPieces rows further on
+                uint4 v[kTurns];
+#pragma unroll
+                for (int z = 0; z < kTurns; ++z) v[z] = *reinterpret_cast<const uint4 *>(from + z * (64 / kPieces) * pitch);
+#pragma unroll
+                for (int z = 0; z < kTurns; ++z, to += hop)
+                    if (r0 + z * (64 / kPieces) < rows) *reinterpret_cast<uint4 *>(to) = v[z];
+            } else {      // an element per lane: rows that start anywhere, the last columns
+                using T = std::conditional_t<type == EF_F32, float, uint16_t>;
+                const int cols = min(kCols, n_end - col0);
                 for (int r = 0; r < rows; r += 8)
 #pragma unroll
                     for (int c = lane; c < kCols; c += 64) {
@@ -208,12 +214,11 @@ __global__ __launch_bounds__(256, RA *RB >= 16 ? 1 : 2) void q8_tiled_kernel(Q8A
                         for (int q = 0; q < 8; ++q)
                             if (c < cols && r + q < rows) reinterpret_cast<T *>(to)[(size_t)(r + q) * p.ldo + c] = v[q];
                     }
-            };
-            if (size == 4) rows_of(0.f);
-            else rows_of((uint16_t)0);
+            }
+            wave_lds_sync();
         }
-        wave_lds_sync();
-    }
+    };
+    q8_by_type(p.out_type, leave);
 }
 
 template <int R, bool PAIR>
