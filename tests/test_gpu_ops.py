@@ -485,3 +485,33 @@ def test_graph_replays_and_other_streams(T):
             eager(x, z, *sets[0][2:], side)
         torch.cuda.synchronize()
         assert torch.equal(eager.out, want)
+
+
+@pytest.mark.parametrize("T,E,k,d,F,kw", [(1, 8, 2, 256, 96, dict(renorm=True)), (37, 32, 4, 200, 72, dict(sigmoid=True, n_groups=4, groups_kept=2, group_best=2, scale=2.5)),
+                                          (300, 16, 3, 256, 160, {})])
+def test_layer_class(T, E, k, d, F, kw):
+    """Q8Layer quantises as the oracle does, and its output follows from its own routing, codes and roundings."""
+    from paper_2510_26730_amd.q8_layer import Q8Layer
+    gen = torch.Generator().manual_seed(T)
+    w13, w2 = (0.1 * torch.randn(*s, generator=gen).bfloat16() for s in ((E, 2 * F, d), (E, d, F)))
+    x, z = torch.randn(T, d, generator=gen).bfloat16(), torch.randn(T, E, generator=gen)
+    bias = 0.1 * torch.randn(E, generator=gen) if kw.get("sigmoid") else None
+    layer = Q8Layer(w13.cuda(), w2.cuda(), k, T + 5, bias=None if bias is None else bias.cuda(), **kw)
+    out = layer(x.cuda(), z.cuda())
+    r = ops.route_scores(f64(z), None if bias is None else f64(bias), k, **kw)
+    assert np.array_equal(layer.ids.cpu().numpy(), r["ids"])
+    q13, s13 = ops.quant_rows(f64(w13).reshape(-1, d))
+    assert np.array_equal(layer.w13.cpu().numpy().reshape(-1, d), q13) and np.array_equal(f64(layer.s13).reshape(-1), s13)
+    q2, s2 = ops.quant_rows(f64(w2).reshape(-1, F))
+    q, s = ops.quant_rows(f64(x))
+    act = ops.matmul_q8(q, s, q13.reshape(E, 2 * F, d), s13.reshape(E, 2 * F), offsets=r["offsets"], rows=r["perm"] // k, swiglu=True)
+    # from here on the device's activations: their rounding to 16 bits decides codes
+    got = layer._act[:T * k]
+    near(got, act, np.abs(act) * (half_step(torch.bfloat16) + 2.0 ** -16) + 1e-30, "activations")
+    q, s = ops.quant_rows(f64(got))
+    y = ops.matmul_q8(q, s, q2.reshape(E, d, F), s2.reshape(E, d), offsets=r["offsets"])
+    want = ops.combine(y, r["w"], r["inv_perm"])
+    slack = ops.combine(np.abs(y), np.abs(r["w"]), r["inv_perm"]) * (k + 44) * U
+    near(out, want, slack + np.abs(want) * half_step(torch.bfloat16), "layer")
+    with pytest.raises(ef.EfError):
+        layer(torch.zeros(T + 6, d, device="cuda").bfloat16(), torch.zeros(T + 6, E, device="cuda"))
