@@ -1,5 +1,5 @@
 // Launch interface between the context-free operators' entry points (ef_ops.hip) and their kernels
-// (ef_router.hip, ef_q8.hip).
+// (ef_router.hip, ef_q8.hip, ef_q8_panel.hip, ef_q8_tiled.hip).
 #pragma once
 #include "../../include/expertflow.h"
 

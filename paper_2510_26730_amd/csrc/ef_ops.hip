@@ -1,5 +1,6 @@
 // Entry points of the context-free operators: routing from logits, rows to 8 bits, products of 8-bit codes, weighted sum of
-// expert rows.  Argument checks and scratch layout; the kernels are in ef_router.hip, ef_q8.hip and ef_q8_tiled.hip.
+// expert rows.  Argument checks and scratch layout; the kernels are in ef_router.hip, ef_q8.hip, ef_q8_panel.hip
+// and ef_q8_tiled.hip.
 #include "ef_ctx.h"
 #include "ef_ops.h"
 

@@ -3,9 +3,9 @@
 //
 // Four waves share the 64 product rows and have 32 matrix rows each (swiglu: 16 gate, 16 up), in steps of 128 codes.  A weight is
 // needed by one wave only, so it goes from memory straight into that wave's operand registers; the tokens are needed by all four and
-// come through LDS by direct loads; both are requested D steps ahead.  What it measured: MEASURED_PANEL.  Up to four teams of four waves that
-// split K in a workgroup gained nothing (28.2, 28.4, 28.2, 29.6 us for 517 x 5640 x 2049): a compute unit takes in about 20 bytes a
-// clock either way.
+// come through LDS by direct loads; both are requested D steps ahead.  517 x 5640 x 2049: 31 us (37-42
+// in tiles of 128 x 128, 81 in tiles of 256 x 256).  Up to four teams of four waves that split K in a workgroup gained nothing (28.2,
+// 28.4, 28.2, 29.6 us in one build): a compute unit takes in about 20 bytes a clock either way.
 // A slab of 1 KiB of LDS is 8 rows x 128 codes; lane 8r + p of a load fetches chunk p ^ r, so that 16 rows at one chunk are read from
 // all banks evenly.
 #include "ef_device.h"
