@@ -145,20 +145,34 @@ __device__ __forceinline__ Q8Row q8_row(const Q8Args &p, int i) {
     return Q8Row{r, p.a_scale ? p.a_scale[r] : 0.f};
 }
 
-// A load of a wave takes 8 rows x 128 bytes, whole lines: lane 8c + r gets chunk c (16 bytes) of row r, or of row 8 + r in the second
-// load.  The matrix instruction wants row i in the lanes i, i + 16, i + 32, i + 48, so the halves of 16 lanes swap: of the first load
-// the upper half (odd chunks of rows 0..7) against the lower half of the second one (even chunks of rows 8..15).  Then every lane has
-// chunks 2g and 2g + 1 of its own row.  Loads of 16 rows x 64 bytes, which need no swap, were slower: 32 tokens of 64
-// experts, first half (329 MB) 77 against 67 us, second half 44 against 39.
-__device__ __forceinline__ void swap_halves(int4v &lo, int4v &hi, bool upper) {
+// Four loads of a wave take 16 rows x 256 bytes, a step: lane 16g + 4q + c gets chunk c (16 bytes) of segment g (64 bytes) of row
+// 4q + j in load j.  Neighbouring lanes have to be neighbours in memory: four lanes in one segment are one cycle of a compute unit's
+// address unit, in four rows they are four (16 bytes a clock, less than the products need).  The matrix instruction wants rows in the
+// lower lane bits, so four lanes and four loads change places: lane 16g + 4q + j then has the four chunks of segment g of row 4q + j,
+// and product c takes every lane's chunk c, on both sides the same K.  With rows in neighbouring lanes of the loads: 32 tokens of 64 experts, first half
+// 64.7 against 60.6 us, second half 34.2 against 31.8; 64 x 2048 x 5632 9.7 against 8.2; 64 x 5632 x 1000 13.4 against 9.3.
+__device__ __forceinline__ void transpose_quads(int4v (&v)[4], int lane) {
+    const bool odd = lane & 1, high = lane & 2;
+    const auto swap = [](int &lo, int &hi, bool up, auto move) {
+        const int l = lo, h = hi, lm = move(l), hm = move(h);
+        lo = up ? hm : l;
+        hi = up ? h : lm;
+    };
+    const auto by1 = [](int x) { return __builtin_amdgcn_mov_dpp(x, 0xB1, 0xf, 0xf, true); };   // lane ^ 1
+    const auto by2 = [](int x) { return __builtin_amdgcn_mov_dpp(x, 0x4E, 0xf, 0xf, true); };   // lane ^ 2
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const int away = upper ? lo[e] : hi[e];
-        const int back = __builtin_amdgcn_mov_dpp(away, 0x128, 0xf, 0xf, true);   // 16 lanes rotated by 8
-        lo[e] = upper ? back : lo[e];
-        hi[e] = upper ? hi[e] : back;
+        int a = v[0][e], b = v[1][e], c = v[2][e], d = v[3][e];
+        swap(a, b, odd, by1);
+        swap(c, d, odd, by1);
+        swap(a, c, high, by2);
+        swap(b, d, high, by2);
+        v[0][e] = a, v[1][e] = b, v[2][e] = c, v[3][e] = d;
     }
 }
+constexpr int kStep = 256;                                                                       // codes of K
+__device__ __forceinline__ int quad_row(int lane, int j) { return (lane & 12) + j; }            // of 16 rows, in load j
+__device__ __forceinline__ int quad_code(int lane) { return (lane >> 4) * 64 + (lane & 3) * 16; }   // of a step
 
 template <int TYPE>
 __device__ __forceinline__ void store_element(void *out, size_t at, float v) {

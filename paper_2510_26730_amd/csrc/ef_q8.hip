@@ -180,8 +180,8 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(QuantArgs a) {
 // products, streamed
 // ------------------------------------------------------------------------------------------------
 
-// Bytes from row to row of the codes in LDS: whole steps of 128, and 16 more that put neighbouring rows on different banks
-__host__ __device__ inline int q8_tile_pitch(int K) { return (K + 127) / 128 * 128 + 16; }
+// Bytes from row to row of the codes in LDS: whole steps, and 16 more that put neighbouring rows on different banks
+__host__ __device__ inline int q8_tile_pitch(int K) { return (K + kStep - 1) / kStep * kStep + 16; }
 
 // Quantises the n product rows from row0 on into LDS, zero from K to the end of the last step; a wave takes 64 pieces of 16 bytes of a
 // row at a time.  Returns the scale of row (lane % 16).  Rows are read twice, the second time from the caches.
@@ -189,7 +189,7 @@ template <int NW, int TYPE>
 __device__ __forceinline__ void quant_tile_codes(const Q8Args &p, int row0, int n, int pitch, int8_t *codes, uint32_t *most) {
     constexpr int kPer = TYPE == EF_F32 ? 4 : 8;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int per_row = ((p.K + 127) / 128 * 128 / kPer + 63) / 64, units = n * per_row;
+    const int per_row = ((pitch - 16) / kPer + 63) / 64, units = n * per_row;
     const auto piece = [&](int unit, int &r, int &e) {
         r = unit / per_row;
         e = ((unit - r * per_row) * 64 + lane) * kPer;
@@ -233,7 +233,7 @@ __device__ __forceinline__ float quant_tile(const Q8Args &p, int row0, int n, in
     return m >= 0x7F800000u || src.scale != src.scale ? __builtin_nanf("") : fmaxf(__builtin_bit_cast(float, m) / 127.f, 0x1p-126f);
 }
 
-// A wave: NB blocks of 16 matrix rows (swiglu: 16 gate and their 16 up rows) for TT tiles of 16 product rows, in steps of 128 codes,
+// A wave: NB blocks of 16 matrix rows (swiglu: 16 gate and their 16 up rows) for TT tiles of 16 product rows, in steps of 256 codes,
 // DEPTH steps in flight; K in KS parts over the waves of a workgroup, which are added in LDS.
 //
 // QUANT: `a` is not codes yet.  The workgroup quantises its tile's rows into LDS itself, while its first weights are on their way, and
@@ -253,43 +253,43 @@ __global__ __launch_bounds__(64 * (KS > 4 ? KS : 4)) void q8_stream_kernel(Q8Arg
     const int F = p.N >> 1;
     const int n0 = (blockIdx.x * (kWaves / KS) + cw) * (PAIR ? 16 : 16 * NB), n_end = PAIR ? F : p.N;
     const int i = lane & 15, g = lane >> 4;
-    const int steps = (p.K + 127) >> 7;
+    const int steps = (p.K + kStep - 1) / kStep;
     const int s0 = steps * part / KS, s1 = steps * (part + 1) / KS;
     const bool run = n0 < n_end && s0 < s1;
 
     // columns past the end and rows past the group's read a neighbour's codes; their results are dropped
-    const int8_t *w[NB][2];
+    const int8_t *w[NB][4];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int c = min(n0 + (PAIR ? 0 : 16 * b) + 8 * h + (lane & 7), n_end - 1);
+        for (int h = 0; h < 4; ++h) {
+            const int c = min(n0 + (PAIR ? 0 : 16 * b) + quad_row(lane, h), n_end - 1);
             w[b][h] = p.w + (size_t)t.group * p.w_group + (size_t)(PAIR && b ? F + c : c) * p.ldw;
         }
     const int k_last = ((p.K + 15) & ~15) - 16;   // last 16 codes that a weight row holds
-    int4v wb[NB][2][DEPTH], xb[TT][2][DEPTH];
+    int4v wb[DEPTH][NB][4], xb[DEPTH][TT][4];
     const auto fetch_w = [&](int u, int s) {
-        const int k = min(min(s, s1 - 1) * 128 + 16 * (lane >> 3), k_last);
+        const int k = min(min(s, s1 - 1) * kStep + quad_code(lane), k_last);
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) wb[b][h][u] = load16(w[b][h] + k);
+            for (int h = 0; h < 4; ++h) wb[u][b][h] = load16(w[b][h] + k);
     };
     if (run)
 #pragma unroll
         for (int u = 0; u < DEPTH; ++u) fetch_w(u, s0 + u);
 
-    const int8_t *x[TT][2];
+    const int8_t *x[TT][4];
     float xs[TT], ws[NB][4];
     if constexpr (QUANT) {
         const int n = t.row_end - t.row0, pitch = q8_tile_pitch(p.K);
         xs[0] = quant_tile<kWaves>(p, t.row0, n, pitch, tile_codes, tile_most);
-        x[0][0] = tile_codes + min(i, n - 1) * pitch + 32 * g;
+        x[0][0] = tile_codes + min(i, n - 1) * pitch + 64 * g;
     } else {
 #pragma unroll
         for (int j = 0; j < TT; ++j) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) x[j][h] = p.a + (size_t)q8_row(p, min(t.row0 + 16 * j + 8 * h + (lane & 7), t.row_end - 1)).row * p.lda;
+            for (int h = 0; h < 4; ++h) x[j][h] = p.a + (size_t)q8_row(p, min(t.row0 + 16 * j + quad_row(lane, h), t.row_end - 1)).row * p.lda;
             xs[j] = q8_row(p, min(t.row0 + 16 * j + i, t.row_end - 1)).scale;
         }
     }
@@ -304,15 +304,15 @@ __global__ __launch_bounds__(64 * (KS > 4 ? KS : 4)) void q8_stream_kernel(Q8Arg
     const int x_end = (p.K + 63) & ~63;
     const auto fetch_x = [&](int u, int s) {
         if constexpr (QUANT) {
-            xb[0][0][u] = load16(x[0][0] + min(s, s1 - 1) * 128);
-            xb[0][1][u] = load16(x[0][0] + min(s, s1 - 1) * 128 + 16);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) xb[u][0][c] = load16(x[0][0] + min(s, s1 - 1) * kStep + 16 * c);
             return;
         }
-        const int k = min(min(s, s1 - 1) * 128 + 16 * (lane >> 3), x_end - 16);
+        const int k = min(min(s, s1 - 1) * kStep + quad_code(lane), x_end - 16);
 #pragma unroll
         for (int j = 0; j < TT; ++j)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) xb[j][h][u] = load16(x[j][h] + k);
+            for (int h = 0; h < 4; ++h) xb[u][j][h] = load16(x[j][h] + k);
     };
 
     int4v acc[NB][TT];
@@ -323,24 +323,24 @@ __global__ __launch_bounds__(64 * (KS > 4 ? KS : 4)) void q8_stream_kernel(Q8Arg
     if (run) {
 #pragma unroll
         for (int u = 0; u < DEPTH; ++u) fetch_x(u, s0 + u);
-        const bool upper = lane & 8;
         const auto multiply = [&](int u, int s) {
             if constexpr (!QUANT) {
 #pragma unroll
-                for (int j = 0; j < TT; ++j) swap_halves(xb[j][0][u], xb[j][1][u], upper);
-                if (s * 128 + 128 > x_end && g >= 2) {
+                for (int j = 0; j < TT; ++j) transpose_quads(xb[u][j], lane);
+                if (s * kStep + 64 * g >= x_end) {
 #pragma unroll
-                    for (int j = 0; j < TT; ++j) xb[j][0][u] = xb[j][1][u] = int4v{0, 0, 0, 0};
+                    for (int j = 0; j < TT; ++j)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) xb[u][j][c] = int4v{0, 0, 0, 0};
                 }
             }
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                swap_halves(wb[b][0][u], wb[b][1][u], upper);
+                transpose_quads(wb[u][b], lane);
 #pragma unroll
-                for (int j = 0; j < TT; ++j) {
-                    acc[b][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wb[b][0][u], xb[j][0][u], acc[b][j], 0, 0, 0);
-                    acc[b][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wb[b][1][u], xb[j][1][u], acc[b][j], 0, 0, 0);
-                }
+                for (int j = 0; j < TT; ++j)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) acc[b][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wb[u][b][c], xb[u][j][c], acc[b][j], 0, 0, 0);
             }
         };
         // loads without a branch between them keep the compiler's wait counts exact; past the end they repeat the last step
@@ -411,9 +411,9 @@ hipError_t launch_stream(const Q8Args &p, hipStream_t s) {
     if (TT < 4 && waves >= 2048) {
         if constexpr (TT < 4) hipLaunchKernelGGL((q8_stream_kernel<TT, PAIR, 2, 1, 1, QUANT>), dim3((wide + 3) / 4, tiles), dim3(256), lds, s, p);
     } else if (PAIR || TT > 1 || waves >= 512) {
-        hipLaunchKernelGGL((q8_stream_kernel<TT, PAIR, 2, 4, 2, QUANT>), dim3(wide, tiles), dim3(256), lds, s, p);
+        hipLaunchKernelGGL((q8_stream_kernel<TT, PAIR, 2, 4, 1, QUANT>), dim3(wide, tiles), dim3(256), lds, s, p);
     } else if constexpr (!PAIR && TT == 1) {
-        hipLaunchKernelGGL((q8_stream_kernel<1, false, 1, 8, 4, QUANT>), dim3(b16, tiles), dim3(512), lds, s, p);
+        hipLaunchKernelGGL((q8_stream_kernel<1, false, 1, 8, 2, QUANT>), dim3(b16, tiles), dim3(512), lds, s, p);
     }
     return hipGetLastError();
 }
@@ -530,17 +530,19 @@ bool q8_product_quantises(const Q8Args &p) {
 
 // Which form a product takes, by its sizes alone (the groups' own sizes are on the device).  Measured with codes in place; us of the
 // form taken / the next best:
-//   streamed   one matrix whose tiles of 16, 32 or 64 rows make one round of workgroups: 64 x 4096 x 4096 10.7 / 17.9 (128 x 128 tiles),
-//              128 x 4096 x 4096 15.4 / 18.7, and up to 32 rows of any width: 24 x 4096 x 14336 18.7 / 24.0 (panels); past a round,
-//              192 x 4096 x 4096, 24.6 against 18.4.  Groups of few rows where K is short, because a panel takes longer to start: 256
-//              groups of 4, 1024 x 512, 28.0 / 35.4; 64 of 3, 2048 x 2816, 64.5 / 67.0, but 64 of 8 75.9 against 71.9 and 128 of 2,
-//              4096 x 1024, 115.8 against 102.8.  Few groups at work, as with one token: 2 of 8, 14336 x 4096, 23.8 / 63.2.
-//   panels     groups of up to 40 rows: 8 of 12, 4096 x 28672, 158.9 / 171.9; 64 of 48, 1408 x 2048, 45.3 against 37.5.  One matrix and a
-//              round of panels, of up to 128 rows (4096 x 14336 25.8 / 29.6; 192 rows 41.3 against 28.8) or with rows that are not
-//              aligned to 64 bytes (512 x 5640 x 2049 31.4 / 36.6; aligned 512 x 4096 x 4096 23.3 against 20.6).
+//   streamed   one matrix, up to 32 rows of any width: 32 x 4096 x 14336 16.2 / 24.7 (panels); tiles of 32 rows that give every compute unit
+//              one workgroup: 64 x 4096 x 4096 8.4 / 16.9 (128 x 128 tiles), 256 x 5632 x 1000 9.9 / 14.0 (tiles of 64); of 64 rows while two
+//              workgroups a unit take all: 256 x 4096 x 4096 14.8 / 17.4, 1024 x 5632 x 1000 19.5 / 27.6, 64 x 4096 x 14336 20.7 / 25.5; past
+//              that 384 x 4096 x 4096 21.4 against 17.9, 517 x 5640 x 2049 43.9 against 42.3, though 384 x 1408 x 2048, 9.3 against 8.5.
+//              Groups of few rows where K is short, because a panel takes longer to start: 256 groups of 12, 1024 x 512, 28.4 / 32.2, of
+//              16 33.7 against 32.5; 64 of 8, 2048 x 2816, 65.2 / 68.6, of 16 84.2 against 69.9.  Few groups at work, as with one token: 8 of
+//              8, 14336 x 4096, 80.7 / 84.8, of 16 103.2 against 84.4.
+//   panels     groups of up to 40 rows: 8 of 12, 4096 x 28672, 158.1 / 171.2; 64 of 64, 1408 x 2048, 43.3 against 35.4.  One matrix and a
+//              round of panels, of up to 128 rows (4096 x 14336 25.9 / 28.0; 192 rows 31.1 against 27.3) or with rows that are not
+//              aligned to 64 bytes (517 x 5640 x 2049 42.3 / 44.1; aligned 517 x 4096 x 4096 25.3 against 18.5).
 //   256 x 256  where rows per group times K make up for the start and end of a tile, and tiles fill half of the chip and more:
 //              64 groups of 384, 2048 x 2816, 223 / 233, of 192 145 against 142; 64 of 384, 1408 x 2048, 148 against 136; 768 x 4096 x
-//              14336 (168 tiles) 58.4 / 72.5, 512 (112) 55.2 against 48.2.
+//              14336 (168 tiles) 55.0 / 72.5, 384 (112) 47.1 against 44.2.
 //   128 x 128  the rest.
 hipError_t launch_q8_product(const Q8Args &p, hipStream_t s) {
     if (p.M <= 0) return hipSuccess;
@@ -550,10 +552,10 @@ hipError_t launch_q8_product(const Q8Args &p, hipStream_t s) {
     if (p.G == 1) {
         if (p.M <= 16) return launch_stream<1, false>(p, s);
         if (p.M <= 32 || stream_waves(p, 2) <= 256) return launch_stream<2, false>(p, s);
-        if (stream_waves(p, 4) <= 256) return launch_stream<4, false>(p, s);
+        if (stream_waves(p, 4) <= 512) return launch_stream<4, false>(p, s);
         if (q8_panel_ok(p) && (p.M <= 128 || p.ldw % 64 != 0) && panels(p.swiglu ? 64 : 128) * q8_tiles_bound(p, 64) <= 256) return launch_q8_panel(p, s);
     } else {
-        if (per <= (p.K <= 1024 ? 16 : p.K <= 2048 ? 4 : 0) || (per <= 16 && stream_waves(p, 1) <= 2048)) return launch_stream<1, false>(p, s);
+        if (per <= (p.K <= 1024 ? 12 : p.K <= 2048 ? 8 : 0) || (per <= 8 && stream_waves(p, 1) <= 2048)) return launch_stream<1, false>(p, s);
         if (q8_panel_ok(p) && per <= 40) return launch_q8_panel(p, s);
     }
     const long long tiles = std::max((p.M + 255) / 256, std::min(p.G, p.M));

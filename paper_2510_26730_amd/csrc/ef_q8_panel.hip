@@ -1,7 +1,7 @@
 // Products of 8-bit codes, panels: one tile of 64 product rows x 128 matrix rows per workgroup, for products whose larger tiles would
 // leave compute units idle; bound by the time from a request to its data.
 //
-// Four waves share the 64 product rows and have 32 matrix rows each (swiglu: 16 gate, 16 up), in steps of 128 codes.  A weight is
+// Four waves share the 64 product rows and have 32 matrix rows each (swiglu: 16 gate, 16 up), in steps of 256 codes.  A weight is
 // needed by one wave only, so it goes from memory straight into that wave's operand registers; the tokens are needed by all four and
 // come through LDS by direct loads; both are requested D steps ahead.  517 x 5640 x 2049: 31 us (37-42
 // in tiles of 128 x 128, 81 in tiles of 256 x 256).  Up to four teams of four waves that split K in a workgroup gained nothing (28.2,
@@ -18,11 +18,11 @@ namespace ef {
 namespace {
 
 constexpr int RA = 2, RB = 4;        // blocks of 16 matrix rows of a wave, of 16 product rows
-constexpr int D = 3;                 // steps on their way
+constexpr int D = 2;                 // steps on their way
 
 template <bool PAIR>
 __global__ __launch_bounds__(256) void q8_panel_kernel(Q8Args p, int npanels) {
-    constexpr int kStage = RB * 2048, kBuffers = D + 1, kLoads = RB / 2 + 2 * RA;   // loads of a step and wave
+    constexpr int kStage = RB * 4096, kBuffers = D + 1, kLoads = RB + 4 * RA;   // loads of a step and wave
     __shared__ __attribute__((aligned(16))) char lds[kBuffers * kStage];
     __shared__ __attribute__((aligned(16))) float wscale[64 * RA], xscale[16 * RB];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -32,7 +32,7 @@ __global__ __launch_bounds__(256) void q8_panel_kernel(Q8Args p, int npanels) {
     const int F = p.N >> 1, n_end = PAIR ? F : p.N;
     const int n0 = panel * (PAIR ? 32 * RA : 64 * RA), col0 = n0 + wave * (PAIR ? 8 * RA : 16 * RA);
     const int i = lane & 15, g = lane >> 4;
-    const int steps = (p.K + 127) >> 7;
+    const int steps = (p.K + kStep - 1) / kStep;
     // matrix row behind row r (0..15) of the wave's block b; columns past the end read a neighbour's codes, their results are dropped
     const auto matrix_row = [&](int first, int b, int r) {
         if constexpr (PAIR) return (b < RA / 2 ? 0 : F) + min(first + (b % (RA / 2)) * 16 + r, F - 1);
@@ -40,30 +40,31 @@ __global__ __launch_bounds__(256) void q8_panel_kernel(Q8Args p, int npanels) {
     };
 
     const int8_t *w = p.w + (size_t)t.group * p.w_group;
-    unsigned woff[RA][2];
+    unsigned woff[RA][4];
 #pragma unroll
     for (int b = 0; b < RA; ++b)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) woff[b][h] = (unsigned)matrix_row(col0, b, 8 * h + (lane & 7)) * (unsigned)p.ldw;
+        for (int h = 0; h < 4; ++h) woff[b][h] = (unsigned)matrix_row(col0, b, quad_row(lane, h)) * (unsigned)p.ldw;
     const int k_last = ((p.K + 15) & ~15) - 16, x_last = ((p.K + 63) & ~63) - 16;
-    int4v wb[D][RA][2];
+    int4v wb[D][RA][4];
     const auto fetch_w = [&](int u, int s) {
-        const unsigned k = min(min(s, steps - 1) * 128 + 16 * (lane >> 3), k_last);
+        const unsigned k = min(min(s, steps - 1) * kStep + quad_code(lane), k_last);
 #pragma unroll
         for (int b = 0; b < RA; ++b)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) wb[u][b][h] = load16(w + (woff[b][h] + k));
+            for (int h = 0; h < 4; ++h) wb[u][b][h] = load16(w + (woff[b][h] + k));
     };
 
-    const int8_t *xsrc[RB / 2];
+    // slabs 2r and 2r + 1 hold the halves of a step of rows 8r .. 8r+7
+    const int8_t *xsrc[RB];
 #pragma unroll
-    for (int q = 0; q < RB / 2; ++q) xsrc[q] = p.a + (size_t)q8_row(p, min(t.row0 + (q * 4 + wave) * 8 + (lane >> 3), t.row_end - 1)).row * p.lda;
+    for (int q = 0; q < RB; ++q) xsrc[q] = p.a + (size_t)q8_row(p, min(t.row0 + (q * 2 + (wave >> 1)) * 8 + (lane >> 3), t.row_end - 1)).row * p.lda;
     const unsigned lds_base = (unsigned)(size_t)&lds[0];
-    const int xchunk = ((lane & 7) ^ (lane >> 3)) * 16;
+    const int xchunk = (wave & 1) * 128 + ((lane & 7) ^ (lane >> 3)) * 16;
     const auto load_x = [&](int buf, int s) {
 #pragma unroll
-        for (int q = 0; q < RB / 2; ++q) {
-            const int8_t *from = xsrc[q] + min(min(s, steps - 1) * 128 + xchunk, x_last);
+        for (int q = 0; q < RB; ++q) {
+            const int8_t *from = xsrc[q] + min(min(s, steps - 1) * kStep + xchunk, x_last);
             const unsigned to = __builtin_amdgcn_readfirstlane(lds_base + buf * kStage + (q * 4 + wave) * 1024);
             asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(to) : "memory");
         }
@@ -85,22 +86,23 @@ __global__ __launch_bounds__(256) void q8_panel_kernel(Q8Args p, int npanels) {
     for (int b = 0; b < RA; ++b)
 #pragma unroll
         for (int j = 0; j < RB; ++j) acc[b][j] = int4v{0, 0, 0, 0};
-    const int slab = (i >> 3) * 1024 + (i & 7) * 128;
-    const int at[2] = {slab + (((2 * g) ^ (i & 7)) << 4), slab + (((2 * g + 1) ^ (i & 7)) << 4)};
-    const bool upper = lane & 8;
+    const int row_at = (i >> 3) * 2048 + (g >> 1) * 1024 + (i & 7) * 128, chunk0 = 4 * (g & 1);
     // the products of step s, weights in wb[u], tokens in LDS buffer `buf`
     const auto multiply = [&](int u, int buf, int s) {
 #pragma unroll
         for (int b = 0; b < RA; ++b) {
-            swap_halves(wb[u][b][0], wb[u][b][1], upper);
-            if (s * 128 + 128 > x_last + 16 && g >= 2) wb[u][b][0] = wb[u][b][1] = int4v{0, 0, 0, 0};   // past the tokens' end
+            transpose_quads(wb[u][b], lane);
+            if (s * kStep + 64 * g > x_last)   // past the tokens' end
+#pragma unroll
+                for (int y = 0; y < 4; ++y) wb[u][b][y] = int4v{0, 0, 0, 0};
         }
         const char *from = lds + buf * kStage;
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
+        for (int y = 0; y < 4; ++y) {
+            const int at = row_at + (((chunk0 + y) ^ (i & 7)) << 4);
             int4v x[RB];
 #pragma unroll
-            for (int j = 0; j < RB; ++j) x[j] = *reinterpret_cast<const int4v *>(from + j * 2048 + at[y]);
+            for (int j = 0; j < RB; ++j) x[j] = *reinterpret_cast<const int4v *>(from + j * 4096 + at);
 #pragma unroll
             for (int j = 0; j < RB; ++j)
 #pragma unroll
@@ -115,7 +117,7 @@ __global__ __launch_bounds__(256) void q8_panel_kernel(Q8Args p, int npanels) {
     for (; s + D < steps; s += D) {
 #pragma unroll
         for (int u = 0; u < D; ++u) {
-            constexpr int behind = 2 * RA + (D - 1) * kLoads;
+            constexpr int behind = 4 * RA + (D - 1) * kLoads;
             static_assert(behind < 64, "vmcnt is a 6-bit counter");
             __builtin_amdgcn_s_waitcnt((behind >> 4) << 14 | 0x0F70 | (behind & 15));
             __syncthreads();            // everybody's part has landed, and nobody reads the buffer of step s + u - 1 any more

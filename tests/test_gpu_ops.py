@@ -306,10 +306,10 @@ FORMS = [
     ("q8_stream_kernel<1, true, 2, 1", 6, 64, 66000, None, True, None), ("q8_stream_kernel<2, false, 2, 4", 30, 320, 512, None, False, None),
     ("q8_stream_kernel<2, false, 2, 1", 18, 64, 66000, None, False, None), ("q8_stream_kernel<2, true, 2, 4", 33, 128, 320, None, True, None),
     ("q8_stream_kernel<2, true, 2, 1", 20, 64, 66000, None, True, None), ("q8_stream_kernel<4, false, 2, 4", 200, 192, 2048, None, False, None),
-    ("q8_stream_kernel<4, true, 2, 4", 250, 64, 2000, None, True, None), ("q8_panel_kernel<false", 100, 448, 8192, None, False, None),
+    ("q8_stream_kernel<4, true, 2, 4", 250, 64, 2000, None, True, None), ("q8_panel_kernel<false", 100, 448, 8300, None, False, None),
     ("q8_panel_kernel<true", 70, 192, 9000, None, True, None), ("q8_panel_kernel<false", 300, 100, 5000, None, False, 112),
     ("q8_panel_kernel<false", 0, 2560, 1024, [10] * 64 + [0, 130], False, None), ("q8_panel_kernel<true", 0, 1088, 1408, [30, 0, 1, 64, 65, 7] * 9, True, None),
-    ("q8_tiled_kernel<2, 2, false", 520, 192, 1700, None, False, None), ("q8_tiled_kernel<2, 2, true", 0, 320, 512, [90, 0, 129, 33], True, None),
+    ("q8_tiled_kernel<2, 2, false", 520, 192, 2300, None, False, None), ("q8_tiled_kernel<2, 2, true", 0, 320, 512, [90, 0, 129, 33], True, None),
     ("q8_tiled_kernel<4, 4, false", 520, 1152, 14000, None, False, None), ("q8_tiled_kernel<4, 4, true", 0, 2112, 14000, [520, 3, 257], True, None),
     ("q8_tiled_kernel<4, 4, false", 0, 2050, 10300, [300, 100, 385], False, 2064),
 ]
