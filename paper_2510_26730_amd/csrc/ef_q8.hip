@@ -533,13 +533,14 @@ bool q8_product_quantises(const Q8Args &p) {
 //   streamed   one matrix, up to 32 rows of any width: 32 x 4096 x 14336 16.2 / 24.7 (panels); tiles of 32 rows that give every compute unit
 //              one workgroup: 64 x 4096 x 4096 8.4 / 16.9 (128 x 128 tiles), 256 x 5632 x 1000 9.9 / 14.0 (tiles of 64); of 64 rows while two
 //              workgroups a unit take all: 256 x 4096 x 4096 14.8 / 17.4, 1024 x 5632 x 1000 19.5 / 27.6, 64 x 4096 x 14336 20.7 / 25.5; past
-//              that 384 x 4096 x 4096 21.4 against 17.9, 517 x 5640 x 2049 43.9 against 42.3, though 384 x 1408 x 2048, 9.3 against 8.5.
+//              that 384 x 4096 x 4096 21.4 against 17.0, 517 x 5640 x 2049 43.9 against 35.0, though 384 x 1408 x 2048, 9.3 against 8.5.
 //              Groups of few rows where K is short, because a panel takes longer to start: 256 groups of 12, 1024 x 512, 28.4 / 32.2, of
 //              16 33.7 against 32.5; 64 of 8, 2048 x 2816, 65.2 / 68.6, of 16 84.2 against 69.9.  Few groups at work, as with one token: 8 of
 //              8, 14336 x 4096, 80.7 / 84.8, of 16 103.2 against 84.4.
-//   panels     groups of up to 40 rows: 8 of 12, 4096 x 28672, 158.1 / 171.2; 64 of 64, 1408 x 2048, 43.3 against 35.4.  One matrix and a
-//              round of panels, of up to 128 rows (4096 x 14336 25.9 / 28.0; 192 rows 31.1 against 27.3) or with rows that are not
-//              aligned to 64 bytes (517 x 5640 x 2049 42.3 / 44.1; aligned 517 x 4096 x 4096 25.3 against 18.5).
+//   panels     groups of up to 40 rows: 8 of 12, 4096 x 28672, 158.1 / 171.2; 64 of 64, 1408 x 2048, 43.3 against 35.4.  One matrix and one
+//              round of panels, of up to 128 rows (4096 x 14336 21.0 / 28.0; 192 rows, two rounds, 31.1 against 27.3), with a long K
+//              (384 x 4096 x 4096 17.0 / 18.0, 2048 x 5632 x 1000 23.1 / 27.2; 768 x 2048 x 2048 11.4 against 11.0) or with rows that are
+//              not aligned to 64 bytes (517 x 5640 x 2049 35.0 / 44.1).
 //   256 x 256  where rows per group times K make up for the start and end of a tile, and tiles fill half of the chip and more:
 //              64 groups of 384, 2048 x 2816, 223 / 233, of 192 145 against 142; 64 of 384, 1408 x 2048, 148 against 136; 768 x 4096 x
 //              14336 (168 tiles) 55.0 / 72.5, 384 (112) 47.1 against 44.2.
@@ -553,7 +554,9 @@ hipError_t launch_q8_product(const Q8Args &p, hipStream_t s) {
         if (p.M <= 16) return launch_stream<1, false>(p, s);
         if (p.M <= 32 || stream_waves(p, 2) <= 256) return launch_stream<2, false>(p, s);
         if (stream_waves(p, 4) <= 512) return launch_stream<4, false>(p, s);
-        if (q8_panel_ok(p) && (p.M <= 128 || p.ldw % 64 != 0) && panels(p.swiglu ? 64 : 128) * q8_tiles_bound(p, 64) <= 256) return launch_q8_panel(p, s);
+        if (q8_panel_ok(p) && (p.M <= 128 || p.K >= 4096 || p.ldw % 64 != 0) &&
+            panels(p.swiglu ? 64 : 128) * q8_tiles_bound(p, 64) <= 256)
+            return launch_q8_panel(p, s);
     } else {
         if (per <= (p.K <= 1024 ? 12 : p.K <= 2048 ? 8 : 0) || (per <= 8 && stream_waves(p, 1) <= 2048)) return launch_stream<1, false>(p, s);
         if (q8_panel_ok(p) && per <= 40) return launch_q8_panel(p, s);
