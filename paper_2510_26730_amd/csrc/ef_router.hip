@@ -9,7 +9,9 @@
 // exact where logits have 16 bits), can hide which of two close values is larger.  That matters at a border only: the last expert
 // chosen against the best left out, the last group kept against the best dropped.  A token whose border is closer than the error is
 // decided again by the whole wave, from its logits' full bits or from scores in 64 bits ("exact" below): with 256 experts some
-// tokens in a thousand.  Groups that 16 lanes cannot share evenly go that way always.
+// tokens in a thousand.  More than 16 groups go that way always, and so do groups of more than
+// 32 experts a lane.  Groups that do not fill their lanes leave the rest empty: 32768 tokens of 200 experts in 8 groups 42 us, 124 with a
+// wave per token.
 //
 // Bound by issuing instructions, ~300 vector ones per token of 256 experts (sigmoid, bias, eight groups, top 8): 32768 tokens 32 us, 64
 // tokens 13 us on the one compute unit that keeps their grouping in the launch.
@@ -285,14 +287,22 @@ constexpr uint32_t kIndexBits = 511;      // low bits of a key: 511 - expert
 // Rows of logits (or the bias) come 16 neighbouring lanes after 16 neighbouring quads or elements, go through LDS, and are read
 // back V at a time: a lane that fetched its own V from memory would touch a line of its own with every load, and the address unit
 // takes a line at a time (64 tokens of 256 experts in one workgroup: 31 of 47 thousand cycles went into those loads).
-// Expert e lies at (e / V) * pitch + e % V; `pitch` keeps the lanes' reads on different banks.
+// A group's `size` experts are the V each of 2^shift lanes, the last of which may have fewer; expert e of a group lies at (e / V) * pitch +
+// e % V behind the group's first lane; `pitch` keeps the lanes' reads on different banks.
 struct RowShape {
-    int E, V, pitch;
-    unsigned per_v;       // (e * per_v) >> 16 = e / V for e below 512
-    bool quads;           // four elements at a time: aligned, V and E multiples of four
+    int E, V, pitch, shift, size;
+    unsigned per_v;       // (e * per_v) >> 16 = e / V for e below 512, V up to 32
+    unsigned per_size;    // (e * per_size) >> 20 = e / size for e below 512; 0: lanes have V experts each, or there is one group
+    bool quads;           // four elements at a time: aligned, V, E and size multiples of four
     __device__ __forceinline__ int at(int e) const {
+        int l0 = 0;
+        if (per_size) {
+            const int g = (int)((unsigned)e * per_size >> 20);
+            e -= g * size;
+            l0 = g << shift;
+        }
         const int l = (int)((unsigned)e * per_v >> 16);
-        return l * pitch + e - l * V;
+        return (l0 + l) * pitch + e - l * V;
     }
 };
 template <int TYPE, int VT>
@@ -388,7 +398,7 @@ __global__ __launch_bounds__(64 * NW, VT <= 16 ? 4 : 2) void router_kernel(Route
         // opaque: what follows from a lane's number is worked out in every pass instead of being kept, spilled, over all of them
         int l = lane & 15;
         asm volatile("" : "+v"(l));
-        const int e0 = l * V;
+        const int g0 = shape.per_size ? (l >> shape.shift) * shape.size : 0, e0 = g0 + (shape.per_size ? l & ((1 << shape.shift) - 1) : l) * V;
         float *mine_rows = rows[wave][lane >> 4];
         const int tok = w0 + (lane >> 4);
         const size_t t = (size_t)t0 + min(tok, n - 1);
@@ -401,7 +411,7 @@ __global__ __launch_bounds__(64 * NW, VT <= 16 ? 4 : 2) void router_kernel(Route
         else
 #pragma unroll
             for (int v = 0; v < VT; ++v) b[v] = 0.f;
-        const int own = max(0, min(V, E - e0));      // experts of this lane
+        const int own = max(0, min(V, min(E, g0 + shape.size) - e0));      // experts of this lane
         float m = kMinusInf;
 #pragma unroll
         for (int v = 0; v < VT; ++v) {
@@ -445,7 +455,7 @@ __global__ __launch_bounds__(64 * NW, VT <= 16 ? 4 : 2) void router_kernel(Route
 
         bool near = false, kept = true;
         if (a.r.n_groups > 1) {
-            const int P = 16 / a.r.n_groups;     // lanes of a group
+            const int P = 1 << shape.shift;     // lanes of a group; those behind the last group have no experts and lose to every group
             float b1 = kMinusInf, b2 = kMinusInf;
 #pragma unroll
             for (int v = 0; v < VT; ++v) {
@@ -695,14 +705,27 @@ __global__ __launch_bounds__(256) void router_scan_kernel(RouterArgs a) {
     if (tid == 0) a.counts[e] = all;
 }
 
+// How 16 lanes share a token's experts: 2^shift lanes a group, V experts a lane.  More groups than lanes, or more than 32 experts a
+// lane: the exact way.
+struct LaneShares { bool fast; int shift, V; };
+LaneShares lane_shares(const ef_router &r) {
+    int shift = 4;
+    while (shift >= 0 && (r.n_groups << shift) > 16) --shift;
+    const int V = shift < 0 ? 33 : (r.n_experts / r.n_groups + (1 << shift) - 1) >> shift;
+    return V <= 32 ? LaneShares{true, shift, V} : LaneShares{false, 4, (r.n_experts + 15) / 16};
+}
+
 template <int VT>
 hipError_t launch_v(const RouterArgs &a, hipStream_t s) {
-    const int tile = router_tile(a.T), E = a.r.n_experts, V = (E + 15) / 16;
-    const bool fast = a.r.n_groups == 1 || (E % 16 == 0 && 16 % a.r.n_groups == 0);
-    const size_t size = a.type == EF_F32 ? 4 : 2;
-    const bool quads = V % 4 == 0 && E % 4 == 0 && a.ld % 4 == 0 && reinterpret_cast<size_t>(a.logits) % (4 * size) == 0 &&
+    const int tile = router_tile(a.T), E = a.r.n_experts, n = a.r.n_groups, size = n == 1 ? E : E / n;
+    const LaneShares share = lane_shares(a.r);
+    const bool fast = share.fast;
+    const int V = share.V;
+    const size_t bytes = a.type == EF_F32 ? 4 : 2;
+    const bool quads = V % 4 == 0 && E % 4 == 0 && size % 4 == 0 && a.ld % 4 == 0 && reinterpret_cast<size_t>(a.logits) % (4 * bytes) == 0 &&
                        reinterpret_cast<size_t>(a.bias) % 16 == 0;
-    const RowShape shape{E, V, quads ? V + 4 : V | 1, (65536u + V - 1) / V, quads};
+    const unsigned per_size = fast && n > 1 && size != V << share.shift ? ((1u << 20) + size - 1) / size : 0;
+    const RowShape shape{E, V, quads ? V + 4 : V | 1, share.shift, per_size ? size : E, (65536u + V - 1) / V, per_size, quads};
     // one tile: a wave for every four tokens; many: two passes per wave, so that two workgroups fit a compute unit's LDS
     if (tile == 16) hipLaunchKernelGGL((router_kernel<VT, 16, 4>), dim3(a.ntiles), dim3(256), 0, s, a, shape, fast);
     else if (a.ntiles == 1) hipLaunchKernelGGL((router_kernel<VT, 64, 16>), dim3(1), dim3(1024), 0, s, a, shape, fast);
@@ -727,7 +750,8 @@ hipError_t launch_router(const RouterArgs &a, hipStream_t s) {
         return e != hipSuccess ? e : launch_fill_i32(a.offsets, E + 1, 0, s);
     }
     if (a.ntiles != (a.T + router_tile(a.T) - 1) / router_tile(a.T) || a.pitch < E || a.pitch % 4 != 0) return hipErrorInvalidValue;
-    return E <= 64 ? launch_v<4>(a, s) : E <= 128 ? launch_v<8>(a, s) : E <= 256 ? launch_v<16>(a, s) : launch_v<32>(a, s);
+    const int V = lane_shares(a.r).V;
+    return V <= 4 ? launch_v<4>(a, s) : V <= 8 ? launch_v<8>(a, s) : V <= 16 ? launch_v<16>(a, s) : launch_v<32>(a, s);
 }
 
 }  // namespace ef

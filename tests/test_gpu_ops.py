@@ -85,6 +85,13 @@ ROUTES = [
     (66000, 20, 3, "bf16", dict(renorm=True)), (77, 48, 4, "f16", dict(sigmoid=True, n_groups=16, groups_kept=7)),
     (50, 64, 16, "bf16", dict(n_groups=2, groups_kept=2, group_best=2)), (30, 256, 8, "bf16", dict(renorm=True)),
     (21, 496, 16, "f16", dict(sigmoid=True, n_groups=8, groups_kept=3, group_best=2)),
+    # groups that do not fill their lanes, of one lane, more lanes than groups need, and more experts than a lane can have
+    (90, 84, 7, "bf16", dict(n_groups=4, groups_kept=2)), (64, 250, 8, "f32", dict(sigmoid=True, n_groups=2, groups_kept=1, group_best=2)),
+    (1100, 200, 8, "f32", dict(sigmoid=True, n_groups=8, groups_kept=4, group_best=2, renorm=True)), (65, 33, 3, "f16", dict(n_groups=3, groups_kept=2)),
+    (130, 90, 5, "f32", dict(sigmoid=True, n_groups=5, groups_kept=2, group_best=2)), (40, 36, 4, "bf16", dict(n_groups=12, groups_kept=5)),
+    (50, 189, 6, "f32", dict(n_groups=9, groups_kept=4, group_best=2)), (33, 504, 8, "f32", dict(sigmoid=True, n_groups=9, groups_kept=3)),
+    (5, 500, 9, "bf16", dict(n_groups=2, groups_kept=2)), (70, 14, 2, "f32", dict(n_groups=14, groups_kept=7)),
+    (47, 300, 8, "f32", dict(sigmoid=True, n_groups=6, groups_kept=3, group_best=2)), (80, 92, 4, "f32", dict(n_groups=4, groups_kept=3, group_best=2)),
 ]
 
 
