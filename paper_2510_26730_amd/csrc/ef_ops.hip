@@ -33,10 +33,13 @@ const char *router_fault(const ef_router *r) {
 }
 bool router_tokens_ok(const ef_router *r, int T) { return T >= 0 && (long long)T * r->top_k <= 0x7FFFFFFFll; }
 
-int router_tiles(int T) { return (T + ef::router_tile(T) - 1) / ef::router_tile(T); }
+int router_tiles(const ef_router *r, int T) {
+    const int tile = ef::router_tile(*r, T);
+    return (T + tile - 1) / tile;
+}
 int router_pitch(const ef_router *r) { return (r->n_experts + 15) / 16 * 16; }
-size_t router_counts_bytes(const ef_router *r, int T) { return rounded((size_t)router_pitch(r) * router_tiles(T)); }
-size_t router_prefix_bytes(const ef_router *r, int T) { return router_tiles(T) > ef::kRouterSumTiles ? 4 * router_counts_bytes(r, T) : 0; }
+size_t router_counts_bytes(const ef_router *r, int T) { return rounded((size_t)router_pitch(r) * router_tiles(r, T)); }
+size_t router_prefix_bytes(const ef_router *r, int T) { return router_tiles(r, T) > ef::kRouterSumTiles ? 4 * router_counts_bytes(r, T) : 0; }
 
 }  // namespace
 
@@ -74,7 +77,7 @@ extern "C" int ef_route_scores(const ef_router *r, const void *logits, int type,
     a.offsets = offsets;
     a.perm = perm;
     a.inv_perm = inv_perm;
-    a.ntiles = router_tiles(T);
+    a.ntiles = router_tiles(r, T);
     a.tile_counts = static_cast<uint8_t *>(work);
     a.pitch = router_pitch(r);
     a.prefix = router_prefix_bytes(r, T) ? reinterpret_cast<int32_t *>(a.tile_counts + router_counts_bytes(r, T)) : nullptr;

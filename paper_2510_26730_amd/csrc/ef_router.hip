@@ -13,8 +13,8 @@
 // 32 experts a lane.  Groups that do not fill their lanes leave the rest empty: 32768 tokens of 200 experts in 8 groups 42 us, 124 with a
 // wave per token.
 //
-// Bound by issuing instructions, ~300 vector ones per token of 256 experts (sigmoid, bias, eight groups, top 8): 32768 tokens 32 us, 64
-// tokens 13 us on the one compute unit that keeps their grouping in the launch.
+// Bound by issuing instructions, ~300 vector ones per token of 256 experts (sigmoid, bias, eight groups, top 8): 32768 tokens 32 us, 48
+// tokens 12 us on the one compute unit that keeps their grouping in the launch.
 //
 // Grouping: a workgroup takes one tile of 16 or 64 tokens, and every expert has a bit per token of the tile in LDS.  The bits
 // below a token's own are its rank among the tile's assignments to that expert, their number the tile's count.  One tile:
@@ -717,7 +717,7 @@ LaneShares lane_shares(const ef_router &r) {
 
 template <int VT>
 hipError_t launch_v(const RouterArgs &a, hipStream_t s) {
-    const int tile = router_tile(a.T), E = a.r.n_experts, n = a.r.n_groups, size = n == 1 ? E : E / n;
+    const int tile = router_tile(a.r, a.T), E = a.r.n_experts, n = a.r.n_groups, size = n == 1 ? E : E / n;
     const LaneShares share = lane_shares(a.r);
     const bool fast = share.fast;
     const int V = share.V;
@@ -726,10 +726,10 @@ hipError_t launch_v(const RouterArgs &a, hipStream_t s) {
                        reinterpret_cast<size_t>(a.bias) % 16 == 0;
     const unsigned per_size = fast && n > 1 && size != V << share.shift ? ((1u << 20) + size - 1) / size : 0;
     const RowShape shape{E, V, quads ? V + 4 : V | 1, share.shift, per_size ? size : E, (65536u + V - 1) / V, per_size, quads};
-    // one tile: a wave for every four tokens; many: two passes per wave, so that two workgroups fit a compute unit's LDS
+    // one tile of 64: a wave for every four tokens; many: two passes per wave, so that two workgroups fit a compute unit's LDS
     if (tile == 16) hipLaunchKernelGGL((router_kernel<VT, 16, 4>), dim3(a.ntiles), dim3(256), 0, s, a, shape, fast);
-    else if (a.ntiles == 1) hipLaunchKernelGGL((router_kernel<VT, 64, 16>), dim3(1), dim3(1024), 0, s, a, shape, fast);
-    else hipLaunchKernelGGL((router_kernel<VT, 64, 8>), dim3(a.ntiles), dim3(512), 0, s, a, shape, fast);
+    else if (VT > 16 || a.ntiles > 1) hipLaunchKernelGGL((router_kernel<VT, 64, 8>), dim3(a.ntiles), dim3(512), 0, s, a, shape, fast);
+    else if constexpr (VT <= 16) hipLaunchKernelGGL((router_kernel<VT, 64, 16>), dim3(1), dim3(1024), 0, s, a, shape, fast);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.ntiles == 1) return e;
     const bool scan = a.prefix != nullptr;
@@ -740,8 +740,13 @@ hipError_t launch_v(const RouterArgs &a, hipStream_t s) {
 
 }  // namespace
 
-// up to 64 tokens are one tile (one launch); beyond, tiles of 16 until the grid of 64s fills the chip
-int router_tile(int T) { return T > 64 && T <= 8192 ? 16 : 64; }
+// Up to 64 tokens are one tile (one launch, on one compute unit); beyond, tiles of 16 until the grid of 64s fills the chip.  With many
+// experts a lane a second launch costs less than the one unit: 64 tokens of 256 experts in 8 groups 11.8 us against 13.7 (48: 11.6
+// against 11.9), of 200 10.6 against 10.0; 17 of 512 13.4 against 16.4.
+int router_tile(const ef_router &r, int T) {
+    const int V = lane_shares(r).V;
+    return T > (V > 16 ? 0 : V > 13 ? 48 : 64) && T <= 8192 ? 16 : 64;
+}
 
 hipError_t launch_router(const RouterArgs &a, hipStream_t s) {
     const int E = a.r.n_experts;
@@ -749,7 +754,8 @@ hipError_t launch_router(const RouterArgs &a, hipStream_t s) {
         const hipError_t e = launch_fill_i32(a.counts, E, 0, s);
         return e != hipSuccess ? e : launch_fill_i32(a.offsets, E + 1, 0, s);
     }
-    if (a.ntiles != (a.T + router_tile(a.T) - 1) / router_tile(a.T) || a.pitch < E || a.pitch % 4 != 0) return hipErrorInvalidValue;
+    const int tile = router_tile(a.r, a.T);
+    if (a.ntiles != (a.T + tile - 1) / tile || a.pitch < E || a.pitch % 4 != 0) return hipErrorInvalidValue;
     const int V = lane_shares(a.r).V;
     return V <= 4 ? launch_v<4>(a, s) : V <= 8 ? launch_v<8>(a, s) : V <= 16 ? launch_v<16>(a, s) : launch_v<32>(a, s);
 }
