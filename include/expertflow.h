@@ -608,7 +608,7 @@ typedef struct ef_router {
  *   topk_ids [T,k] i32, topk_w [T,k] f32, counts [E] i32, offsets [E+1] i32, perm, inv_perm [T*k] i32  [dev]
  * T = 0 is allowed (counts and offsets are zeroed); T*k below 2^31.
  */
-size_t ef_route_scores_work(const ef_router *r, int T);   /* 0 if r or T is out of range */
+size_t ef_route_scores_work(const ef_router *r, int T);   /* enough for fewer tokens too; 0 if r or T is out of range */
 int ef_route_scores(const ef_router *r, const void *logits, int type, int64_t ld, const float *bias, int T,
                     int32_t *topk_ids, float *topk_w, int32_t *counts, int32_t *offsets, int32_t *perm,
                     int32_t *inv_perm, void *work, size_t work_bytes, void *stream);
@@ -645,7 +645,8 @@ typedef struct ef_q8_product {
     const int32_t *offsets;   /* [dev] [G+1] or NULL (G = 1: all M rows) */
     const void *w;            /* [dev] i8, 16-byte aligned: G matrices of N rows of K codes, ldw bytes from row to row,
                                  w_group bytes from matrix to matrix, both multiples of 16, ldw >= K rounded up to 16
-                                 (every matrix holds N whole rows of that many readable bytes) */
+                                 (every matrix holds N whole rows of that many readable bytes;
+                                 rows a multiple of 64 bytes apart are read fastest) */
     const float *w_scale;     /* [dev] [G,N] f32 */
     void *out;                /* [dev] M rows of N (swiglu: N/2) elements of out_type, ldo elements from row to row */
     int64_t lda, ldw, w_group, ldo;

@@ -20,14 +20,14 @@ struct RouterArgs {
     int T;
     int32_t *ids;
     float *w;
-    int32_t *counts, *offsets, *perm, *inv_perm;
+    int32_t *counts, *offsets, *perm, *inv_perm;   // inv_perm holds, between the launches, an assignment's rank in its tile
     int ntiles;            // token tiles of router_tile(r, T) tokens
     uint8_t *tile_counts;  // [ntiles][pitch] (scratch): assignments of a tile to an expert
     int pitch;             // E rounded up to 16
     int32_t *prefix;       // [ntiles][pitch] (scratch): their prefixes over the tiles; null for up to kRouterSumTiles tiles
-    uint8_t *rank;         // [T*k] (scratch): earlier tokens of the tile with the same expert
 };
 int router_tile(const ef_router &r, int T);
+constexpr int kRouterSmallTiles = 8192;   // most tokens that are in tiles of 16
 hipError_t launch_router(const RouterArgs &a, hipStream_t s);
 
 // ---- 8-bit products (ef_q8.hip) ----------------------------------------------------------------

@@ -45,7 +45,8 @@ size_t router_prefix_bytes(const ef_router *r, int T) { return router_tiles(r, T
 
 extern "C" size_t ef_route_scores_work(const ef_router *r, int T) {
     if (router_fault(r) || !router_tokens_ok(r, T)) return 0;
-    return router_counts_bytes(r, T) + router_prefix_bytes(r, T) + rounded((size_t)T * r->top_k) + kAlign;
+    const auto bytes = [&](int t) { return router_counts_bytes(r, t) + router_prefix_bytes(r, t) + kAlign; };
+    return std::max(bytes(T), bytes(std::min(T, ef::kRouterSmallTiles)));   // fewer tokens never need more
 }
 
 extern "C" int ef_route_scores(const ef_router *r, const void *logits, int type, int64_t ld, const float *bias, int T,
@@ -81,7 +82,6 @@ extern "C" int ef_route_scores(const ef_router *r, const void *logits, int type,
     a.tile_counts = static_cast<uint8_t *>(work);
     a.pitch = router_pitch(r);
     a.prefix = router_prefix_bytes(r, T) ? reinterpret_cast<int32_t *>(a.tile_counts + router_counts_bytes(r, T)) : nullptr;
-    a.rank = a.tile_counts + router_counts_bytes(r, T) + router_prefix_bytes(r, T);
     EF_HIP(nullptr, ef::launch_router(a, static_cast<hipStream_t>(stream)));
     return EF_OK;
 }

@@ -573,7 +573,7 @@ __global__ __launch_bounds__(64 * NW, VT <= 16 ? 4 : 2) void router_kernel(Route
     if (a.ntiles > 1) {
         for (int e = tid; e < a.pitch; e += kThreads) a.tile_counts[(size_t)blockIdx.x * a.pitch + e] = (uint8_t)__popcll(bits[e]);
         for (int x = tid; x < n * k; x += kThreads)
-            a.rank[(size_t)t0 * k + x] = (uint8_t)__popcll(bits[chosen_ids[x]] & (((Bits)1 << (x / k)) - 1));
+            a.inv_perm[(size_t)t0 * k + x] = __popcll(bits[chosen_ids[x]] & (((Bits)1 << (x / k)) - 1));
         return;
     }
     if (wave == 0) {
@@ -678,7 +678,7 @@ __global__ __launch_bounds__(256) void router_scatter_kernel(RouterArgs a, int t
     const size_t a0 = (size_t)blockIdx.x * tile * k;
     const int n = min(tile, a.T - (int)blockIdx.x * tile) * k;
     for (int x = tid; x < n; x += 256) {
-        const int pos = first[a.ids[a0 + x]] + a.rank[a0 + x];
+        const int pos = first[a.ids[a0 + x]] + a.inv_perm[a0 + x];     // its rank in the tile, from the first launch
         a.perm[pos] = (int)(a0 + x);
         a.inv_perm[a0 + x] = pos;
     }
@@ -745,7 +745,7 @@ hipError_t launch_v(const RouterArgs &a, hipStream_t s) {
 // against 11.9), of 200 10.6 against 10.0; 17 of 512 13.4 against 16.4.
 int router_tile(const ef_router &r, int T) {
     const int V = lane_shares(r).V;
-    return T > (V > 16 ? 0 : V > 13 ? 48 : 64) && T <= 8192 ? 16 : 64;
+    return T > (V > 16 ? 0 : V > 13 ? 48 : 64) && T <= kRouterSmallTiles ? 16 : 64;
 }
 
 hipError_t launch_router(const RouterArgs &a, hipStream_t s) {

@@ -54,6 +54,12 @@ def test_router_of_groups_is_checked():
     refused(route(router(n_experts=32, top_k=17), ld=32), "top_k")
     assert ef.ef_route_scores_work(4, 8, 2) > 0 and ef.ef_route_scores_work(-1, 8, 2) == 0
     assert ef.ef_route_scores_work(1 << 30, 512, 16) == 0
+    # scratch for a number of tokens is enough for fewer, and small: counts of 16 tokens and their prefixes, a byte or five an expert
+    for E, k, groups in ((8, 8, 1), (84, 7, 4), (200, 4, 8), (256, 8, 8), (512, 16, 1)):
+        sizes = [ef.ef_route_scores_work(T, E, k, groups, groups) for T in (0, 1, 16, 17, 48, 49, 64, 65, 100, 4096, 8192, 8193, 20000, 32768, 65536, 65537, 200000)]
+        assert sizes == sorted(sizes)
+        assert ef.ef_route_scores_work(32768, E, k, groups, groups) <= 4096 + 16 * E * (32768 // 16)
+        assert ef.ef_route_scores_work(8192, E, k, groups, groups) <= 4096 + (E + 15) // 16 * 8192
 
 
 @pytest.mark.parametrize("kw,word", [
