@@ -8,7 +8,7 @@
 // p ^ fold(r) of its row instead of p: the 16-byte chunks of a slab lie permuted within their row, and a read of 32 rows at one
 // chunk touches all banks evenly.
 // The results go through LDS on their way out, so that a wave stores whole runs of a row.
-// What it measured: 8192 x 4096 x 14336 in tiles of 256 x 256 444-495 us, 1.95-2.17 POP/s; the same kernel without its loads took 82 % of
+// What it measured: 8192 x 4096 x 14336 in tiles of 256 x 256 444-509 us, 1.9-2.17 POP/s; the same kernel without its loads took 82 % of
 // that, with its matrix products alone 63 %.  1056 tokens x 6 of 64 experts, 1408 -> 2048, in tiles of 128 x 128: 67 us.
 #include "ef_device.h"
 #include "ef_kernels.h"

@@ -17,9 +17,9 @@ from . import binding as ef
 
 
 def quantise(w):
-    """Weights [.., N, K] on the device -> codes int8 of the same shape, rows 16-byte aligned, and scales [.., N]."""
+    """Weights [.., N, K] on the device -> codes int8 of the same shape, rows 64 bytes aligned (read faster than at 16), and scales [.., N]."""
     *lead, K = w.shape
-    codes = torch.empty(*lead, (K + 15) // 16 * 16, dtype=torch.int8, device=w.device)
+    codes = torch.empty(*lead, (K + 63) // 64 * 64, dtype=torch.int8, device=w.device)
     scales = torch.empty(*lead, dtype=torch.float32, device=w.device)
     ef.ef_quant_rows(w.reshape(-1, K), codes.view(-1, codes.shape[-1]), scales.view(-1), stream=torch.cuda.current_stream(w.device))
     return codes[..., :K], scales
