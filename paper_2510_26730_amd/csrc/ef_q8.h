@@ -149,8 +149,9 @@ __device__ __forceinline__ Q8Row q8_row(const Q8Args &p, int i) {
 // 4q + j in load j.  Neighbouring lanes have to be neighbours in memory: four lanes in one segment are one cycle of a compute unit's
 // address unit, in four rows they are four (16 bytes a clock, less than the products need).  The matrix instruction wants rows in the
 // lower lane bits, so four lanes and four loads change places: lane 16g + 4q + j then has the four chunks of segment g of row 4q + j,
-// and product c takes every lane's chunk c, on both sides the same K.  With rows in neighbouring lanes of the loads: 32 tokens of 64 experts, first half
-// 64.7 against 60.6 us, second half 34.2 against 31.8; 64 x 2048 x 5632 9.7 against 8.2; 64 x 5632 x 1000 13.4 against 9.3.
+// and product c takes every lane's chunk c, on both sides the same K.  With rows in neighbouring lanes of the loads: 32
+// tokens of 64 experts, first half 64.7 against 60.6 us, second half 34.2 against 31.8; 64 x 2048 x 5632 9.7 against 8.2; 64 x 5632 x 1000
+// 13.4 against 9.3.
 __device__ __forceinline__ void transpose_quads(int4v (&v)[4], int lane) {
     const bool odd = lane & 1, high = lane & 2;
     const auto swap = [](int &lo, int &hi, bool up, auto move) {

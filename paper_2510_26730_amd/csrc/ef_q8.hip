@@ -4,7 +4,7 @@
 // (K <= 131071), so neither the split of K nor the order of its parts changes a bit.  Three forms, all reading the codes as the
 // caller has them, row by row:
 //   streamed (here): few rows per matrix, bound by reading the weights.  Operands go from memory straight into the registers of
-//   v_mfma_i32_16x16x64_i8; a load of a wave covers whole lines, 128 bytes of 8 rows (ef_q8.h says how that becomes operands).
+//   v_mfma_i32_16x16x64_i8; a load of a wave covers 256 bytes of 4 rows (ef_q8.h says how that becomes operands).
 //   panels (ef_q8_panel.hip): too few tiles to fill the chip, or groups of some tens of rows.
 //   tiled (ef_q8_tiled.hip): many rows, bound by the matrix cores.
 #include "ef_device.h"
@@ -520,7 +520,7 @@ hipError_t launch_quant_rows(const QuantArgs &a, hipStream_t s) {
 }
 
 // Whether the product quantises rows itself (p.a: the rows as they are): up to four rows, one matrix, aligned to 16 bytes, whose codes
-// fit LDS.  1 x 4096 x 4096: 7 us in one launch against 3 + 6 and the gap between two.  Not for groups, whose tiles need LDS for 16
+// fit LDS.  1 x 4096 x 4096: 6.4 us in one launch against 3 + 6 and the gap between two.  Not for groups, whose tiles need LDS for 16
 // rows each and run four instead of five to a compute unit: 32 tokens of 64 experts, first half, 74 against 4.6 + 64.5 us.
 bool q8_product_quantises(const Q8Args &p) {
     const int per = p.a_type == EF_F32 ? 4 : 8;
