@@ -621,9 +621,13 @@ int ef_route_scores(const ef_router *r, const void *logits, int type, int64_t ld
  *   x [dev] rows of K elements of `type` (EF_BF16, EF_F16, EF_F32), ldx elements from row to row;
  *   codes [dev] i8, ldc bytes from row to row, the bytes from K up to the next multiple of 64, as far as ldc
  *   reaches, are zeroed; scales [dev] [rows] f32.  rows = 0 is allowed.
+ * ef_quant_rows_within: codes are columns of a wider matrix; a row's first `width` bytes (K <= width <= ldc) may be
+ * written, and are zeroed so far only.
  */
 int ef_quant_rows(const void *x, int type, int64_t ldx, int rows, int K, int8_t *codes, int64_t ldc, float *scales,
                   void *stream);
+int ef_quant_rows_within(const void *x, int type, int64_t ldx, int rows, int K, int8_t *codes, int64_t width, int64_t ldc,
+                         float *scales, void *stream);
 
 /*
  * Products of 8-bit codes with a scale for every token and every output channel, for one matrix or for the

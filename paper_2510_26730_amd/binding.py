@@ -37,7 +37,7 @@ EXPORTS = [
     "ef_delta_cache_create", "ef_delta_cache_destroy", "ef_delta_cache_put", "ef_delta_cache_get",
     "ef_delta_cache_counts", "ef_delta_producer_create", "ef_delta_producer_destroy", "ef_delta_submit",
     "ef_delta_drain", "ef_delta_assemble",
-    "ef_route_scores_work", "ef_route_scores", "ef_quant_rows", "ef_matmul_q8_work", "ef_matmul_q8", "ef_combine",
+    "ef_route_scores_work", "ef_route_scores", "ef_quant_rows", "ef_quant_rows_within", "ef_matmul_q8_work", "ef_matmul_q8", "ef_combine",
 ]
 EF_BF16, EF_F16, EF_F32, EF_I8 = 0, 1, 2, 3
 EF_SCORE_SOFTMAX, EF_SCORE_SIGMOID = 0, 1
@@ -178,6 +178,7 @@ def lib():
         L.ef_route_scores_work.argtypes = [vp, i32]
         L.ef_route_scores.argtypes = [vp, vp, i32, i64, vp, i32, vp, vp, vp, vp, vp, vp, vp, szt, vp]
         L.ef_quant_rows.argtypes = [vp, i32, i64, i32, i32, vp, i64, vp, vp]
+        L.ef_quant_rows_within.argtypes = [vp, i32, i64, i32, i32, vp, i64, i64, vp, vp]
         L.ef_matmul_q8_work.restype = szt
         L.ef_matmul_q8_work.argtypes = [vp]
         L.ef_matmul_q8.argtypes = [vp, vp, szt, vp]
@@ -622,15 +623,14 @@ def ef_route_scores(logits, bias, ids, w, counts, offsets, perm, inv_perm, work,
 
 
 def ef_quant_rows(x, codes, scales, stream=None):
-    """Rows of x [rows, K] to int8 codes [rows, >= K] (zeroed up to the next multiple of 64 columns) and scales [rows]."""
+    """Rows of x [rows, K] to int8 codes [rows, >= K] (zeroed up to the next multiple of 64 columns, of those there are) and scales [rows]."""
     xp, kind, ldx = _rows(x)
     cp, ckind, ldc = _rows(codes)
     if ckind != EF_I8 or codes.shape[0] != x.shape[0] or codes.shape[1] < x.shape[1]:
         raise EfError(EF_EINVAL, "ef_quant_rows: codes must be int8 and as large as x")
     if scales.numel() < x.shape[0]:
         raise EfError(EF_EINVAL, "ef_quant_rows: a scale for every row is needed")
-    return _check(None, lib().ef_quant_rows(xp, kind, ldx, x.shape[0], x.shape[1], cp, min(ldc, max(codes.shape[1], x.shape[1])) if x.shape[0] == 1 else ldc,
-                                            _ptr(scales), _stream(stream)))
+    return _check(None, lib().ef_quant_rows_within(xp, kind, ldx, x.shape[0], x.shape[1], cp, codes.shape[1], ldc, _ptr(scales), _stream(stream)))
 
 
 def _product(a, w, w_scale, out, a_scale, rows, row_div, offsets, swiglu):

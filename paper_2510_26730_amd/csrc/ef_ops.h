@@ -37,7 +37,7 @@ struct QuantArgs {
     long long ldx;
     int rows, K;
     int8_t *codes;
-    long long ldc;
+    long long ldc, width;  // bytes from row to row; bytes of a row that may be written
     float *scales;         // null: x are codes already, only padded
 };
 hipError_t launch_quant_rows(const QuantArgs &a, hipStream_t s);

@@ -88,13 +88,19 @@ extern "C" int ef_route_scores(const ef_router *r, const void *logits, int type,
 
 extern "C" int ef_quant_rows(const void *x, int type, int64_t ldx, int rows, int K, int8_t *codes, int64_t ldc, float *scales,
                              void *stream) {
+    return ef_quant_rows_within(x, type, ldx, rows, K, codes, ldc, ldc, scales, stream);
+}
+
+extern "C" int ef_quant_rows_within(const void *x, int type, int64_t ldx, int rows, int K, int8_t *codes, int64_t width, int64_t ldc,
+                                    float *scales, void *stream) {
     if (!is_float_type(type)) return fail(nullptr, EF_EINVAL, "ef_quant_rows: rows of type %d", type);
     if (rows < 0 || K < 1) return fail(nullptr, EF_EINVAL, "ef_quant_rows: %d rows of %d", rows, K);
     if (rows == 0) return EF_OK;
     if (!x || !codes || !scales) return fail(nullptr, EF_EINVAL, "ef_quant_rows: null pointer");
     if (ldx < K || ldc < K) return fail(nullptr, EF_EINVAL, "ef_quant_rows: rows of %d overlap (ldx %lld, ldc %lld)", K, (long long)ldx, (long long)ldc);
+    if (width < K || width > ldc) return fail(nullptr, EF_EINVAL, "ef_quant_rows: width %lld outside K=%d..ldc=%lld", (long long)width, K, (long long)ldc);
     if (!aligned_to_type(x, type) || !aligned4(scales)) return fail(nullptr, EF_EINVAL, "ef_quant_rows: misaligned pointer");
-    const ef::QuantArgs a{x, type, ldx, rows, K, codes, ldc, scales};
+    const ef::QuantArgs a{x, type, ldx, rows, K, codes, ldc, width, scales};
     EF_HIP(nullptr, ef::launch_quant_rows(a, static_cast<hipStream_t>(stream)));
     return EF_OK;
 }
@@ -169,7 +175,7 @@ extern "C" int ef_matmul_q8(const ef_q8_product *p, void *work, size_t work_byte
         if (!ef::q8_product_quantises(q)) {
             int8_t *codes = static_cast<int8_t *>(work);
             float *scales = reinterpret_cast<float *>(codes + rounded((size_t)p->a_rows * q8_pitch(p->K)));
-            const ef::QuantArgs qa{p->a, p->a_type, p->lda, p->a_rows, p->K, codes, q8_pitch(p->K), scales};
+            const ef::QuantArgs qa{p->a, p->a_type, p->lda, p->a_rows, p->K, codes, q8_pitch(p->K), q8_pitch(p->K), scales};
             EF_HIP(nullptr, ef::launch_quant_rows(qa, s));
             q.a = codes;
             q.lda = q8_pitch(p->K);

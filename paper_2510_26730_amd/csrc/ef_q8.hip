@@ -156,7 +156,7 @@ __global__ __launch_bounds__(256) void quant_any_kernel(QuantArgs a) {
     const bool bad = most >= 0x7F800000u;
     const float s = fmaxf(__builtin_bit_cast(float, most) / 127.f, 0x1p-126f), inv = 1.f / s;
     if (tid == 0) a.scales[row] = bad ? __builtin_nanf("") : s;
-    const int padded = (int)min((long long)(a.K + 63) / 64 * 64, a.ldc);
+    const int padded = (int)min((long long)(a.K + 63) / 64 * 64, a.width);
     for (int i0 = 0; i0 < padded; i0 += 8 * 256) {
         T v[8];
 #pragma unroll
@@ -492,7 +492,7 @@ hipError_t launch_quant(const QuantArgs &a, hipStream_t s) {
     constexpr int kPer = TYPE == EF_F32 ? 4 : 8;
     const int pieces = (a.K + kPer - 1) / kPer;      // of 16 bytes
     const bool whole = a.K % kPer == 0 && a.ldx % kPer == 0 && reinterpret_cast<size_t>(a.x) % 16 == 0 && a.ldc % 16 == 0 &&
-                       a.ldc >= (a.K + 63) / 64 * 64 && reinterpret_cast<size_t>(a.codes) % 16 == 0;
+                       a.width >= (a.K + 63) / 64 * 64 && reinterpret_cast<size_t>(a.codes) % 16 == 0;
     const dim3 block(256);
     if (!whole || pieces > 64 * 4 * 16) hipLaunchKernelGGL(quant_any_kernel<TYPE>, dim3(a.rows), block, 0, s, a);
     // a wave per row while that keeps eight pieces of a lane or fewer and there are rows for every compute unit, else four
