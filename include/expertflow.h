@@ -666,7 +666,7 @@ int ef_matmul_q8(const ef_q8_product *p, void *work, size_t work_bytes, void *st
 /*
  * Weighted sum of the expert rows of each token, the last step of a layer made of the calls above:
  * out[t] = sum_j w[t][j] * y[inv_perm[t*k+j]], j ascending, in 32 bits, rounded once.  inv_perm == NULL: the
- * identity.  A row number outside 0..y_rows-1 counts as a row of NaN.
+ * identity.  A row number outside 0..y_rows-1 counts as a row of NaN (y_rows = 0: every one; y is not read then).
  *   y [dev] y_rows rows of d elements of y_type, ldy from row to row; out [dev] [T] rows of d, ldo from row to row
  */
 int ef_combine(const void *y, int y_type, int64_t ldy, int y_rows, const float *w, const int32_t *inv_perm, int T, int k,

@@ -192,7 +192,7 @@ extern "C" int ef_combine(const void *y, int y_type, int64_t ldy, int y_rows, co
     if (!is_float_type(y_type) || !is_float_type(out_type)) return fail(nullptr, EF_EINVAL, "ef_combine: unknown type");
     if (T < 0 || k < 1 || d < 1 || y_rows < 0 || (long long)T * k > 0x7FFFFFFFll) return fail(nullptr, EF_EINVAL, "ef_combine: T, k, d or y_rows out of range");
     if (T == 0) return EF_OK;
-    if (!y || !w || !out) return fail(nullptr, EF_EINVAL, "ef_combine: null pointer");
+    if ((!y && y_rows > 0) || !w || !out) return fail(nullptr, EF_EINVAL, "ef_combine: null pointer");
     if (ldy < d || ldo < d) return fail(nullptr, EF_EINVAL, "ef_combine: rows of %d overlap", d);
     if (!inv_perm && y_rows < (long long)T * k) return fail(nullptr, EF_EINVAL, "ef_combine: %d rows for %d x %d", y_rows, T, k);
     if (!aligned_to_type(y, y_type) || !aligned_to_type(out, out_type) || !aligned4(w) || !aligned4(inv_perm))

@@ -434,10 +434,12 @@ __global__ __launch_bounds__(256) void combine_rows_kernel(CombineArgs a) {
     const int t = blockIdx.x, c = (blockIdx.y * 256 + threadIdx.x) * W;
     if (c >= a.d) return;
     float sum[W];
+    // a row that does not exist reads row 0 and counts as NaN; without rows there is not even that one
+    const int slots = a.y_rows ? a.k : 0;
 #pragma unroll
-    for (int e = 0; e < W; ++e) sum[e] = 0.f;
+    for (int e = 0; e < W; ++e) sum[e] = a.y_rows ? 0.f : __builtin_nanf("");
     const long long slot0 = (long long)t * a.k;
-    for (int j0 = 0; j0 < a.k; j0 += 4) {
+    for (int j0 = 0; j0 < slots; j0 += 4) {
         Y v[4][W];
         float w[4];
         bool live[4];

@@ -30,3 +30,24 @@ def test_codes_in_columns_of_a_wider_matrix(rows, K, first, last, pitch, dtype):
     assert np.array_equal(wide[:, first:first + K].cpu().numpy(), q) and np.array_equal(f64(scales), s)
     assert (wide[:, first + K:first + padded] == 0).all()
     assert (wide[:, :first] == 99).all() and (wide[:, first + padded:] == 99).all() and (room[rows * pitch:] == 99).all()
+
+
+# ---- weighted sum --------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("d,pad", [(8, 0), (33, 3)])
+@pytest.mark.parametrize("y_type", ["bf16", "f32"])
+def test_combine_without_any_row(y_type, d, pad):
+    """No row of y exists: every number of a row is out of range, the sums are NaN, and nothing of y is read."""
+    y = torch.ones(4, d + pad, dtype=TYPES[y_type], device="cuda")
+    inv = torch.tensor([0, 1, -1, 3, 0, 2], dtype=torch.int32, device="cuda")
+    out = torch.full((4, d + pad), 5.0, device="cuda")
+    w = torch.ones(3, 2, device="cuda")
+    for address in (None, y.data_ptr()):
+        out[:] = 5
+        assert ef.lib().ef_combine(address, ef._rows(y)[1], d + pad, 0, w.data_ptr(), inv.data_ptr(), 3, 2, d, out.data_ptr(), ef.EF_F32, d + pad,
+                                   stream().cuda_stream) == ef.EF_OK
+        got = out.cpu()
+        assert got[:3, :d].isnan().all() and (got[3] == 5).all() and (got[:, d:] == 5).all()
+    out[:] = 5
+    ef.ef_combine(y[:0, :d], w, inv, out[:3, :d], stream=stream())
+    assert out[:3, :d].isnan().all() and (out[:, d:] == 5).all()
