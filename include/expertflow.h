@@ -613,6 +613,20 @@ int ef_route_scores(const ef_router *r, const void *logits, int type, int64_t ld
                     int32_t *topk_ids, float *topk_w, int32_t *counts, int32_t *offsets, int32_t *perm,
                     int32_t *inv_perm, void *work, size_t work_bytes, void *stream);
 
+/* The same call with its operands in a structure, for bindings that pay for every argument of a call. */
+typedef struct ef_route_operands {
+    const void *logits;
+    const float *bias;
+    int32_t *topk_ids;
+    float *topk_w;
+    int32_t *counts, *offsets, *perm, *inv_perm;
+    void *work;
+    size_t work_bytes;
+    int64_t ld;
+    int32_t type, T;
+} ef_route_operands;
+int ef_route_scores_of(const ef_router *r, const ef_route_operands *o, void *stream);
+
 /*
  * Rows to 8 bits with a scale each: scale = max(f32(max|x| / 127), 2^-126); code = x / scale rounded to the
  * nearest whole number (ties to even; the quotient itself, not a product with a reciprocal), so codes are in

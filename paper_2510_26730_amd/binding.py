@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import os
+import struct
 
 import numpy as np
 
@@ -37,7 +38,7 @@ EXPORTS = [
     "ef_delta_cache_create", "ef_delta_cache_destroy", "ef_delta_cache_put", "ef_delta_cache_get",
     "ef_delta_cache_counts", "ef_delta_producer_create", "ef_delta_producer_destroy", "ef_delta_submit",
     "ef_delta_drain", "ef_delta_assemble",
-    "ef_route_scores_work", "ef_route_scores", "ef_quant_rows", "ef_quant_rows_within", "ef_matmul_q8_work", "ef_matmul_q8", "ef_combine",
+    "ef_route_scores_work", "ef_route_scores", "ef_route_scores_of", "ef_quant_rows", "ef_quant_rows_within", "ef_matmul_q8_work", "ef_matmul_q8", "ef_combine",
 ]
 EF_BF16, EF_F16, EF_F32, EF_I8 = 0, 1, 2, 3
 EF_SCORE_SOFTMAX, EF_SCORE_SIGMOID = 0, 1
@@ -177,6 +178,7 @@ def lib():
         L.ef_route_scores_work.restype = szt
         L.ef_route_scores_work.argtypes = [vp, i32]
         L.ef_route_scores.argtypes = [vp, vp, i32, i64, vp, i32, vp, vp, vp, vp, vp, vp, vp, szt, vp]
+        L.ef_route_scores_of.argtypes = [vp, vp, vp]
         L.ef_quant_rows.argtypes = [vp, i32, i64, i32, i32, vp, i64, vp, vp]
         L.ef_quant_rows_within.argtypes = [vp, i32, i64, i32, i32, vp, i64, i64, vp, vp]
         L.ef_matmul_q8_work.restype = szt
@@ -579,100 +581,157 @@ def ef_delta_assemble(c, token_ids, tok_off, layer, S, H, L, gain, M, out=None):
 # Two-dimensional operands may have any row stride; their elements of a row are consecutive.
 
 _kinds = {}
+_I32 = _F32 = None      # torch's types
+
+
+def _load_types():
+    global _I32, _F32
+    import torch
+    _I32, _F32 = torch.int32, torch.float32
+    _kinds.update({torch.bfloat16: EF_BF16, torch.float16: EF_F16, torch.float32: EF_F32, torch.int8: EF_I8})
+
+
+def _device(x, what):
+    """The device of a call's first operand, where the others have to be."""
+    device = x.get_device()
+    if device < 0:
+        raise EfError(EF_EINVAL, f"{what}: the operands must be on a GPU")
+    return device
+
+
+def _vector(x, dtype, n, device, what):
+    """Address of at least n consecutive elements of a type on the device (None: on any); None and plain addresses are passed on."""
+    if x is None:
+        return None
+    try:
+        if x.dtype is dtype and x.numel() >= n and x.is_contiguous() and (device is None or x.get_device() == device):
+            return x.data_ptr()
+        is_on = x.device
+    except AttributeError:
+        if isinstance(x, int):
+            return x
+        raise EfError(EF_EINVAL, f"{what} must be a tensor, and is {type(x)}") from None
+    where = "" if device is None else f" on device {device}"
+    raise EfError(EF_EINVAL, f"{what} must hold {n} consecutive elements of {dtype}{where}, and is {tuple(x.shape)} of {x.dtype} on {is_on}")
 
 
 def _rows(x):
-    """(address, type, elements from row to row) of a matrix of tensor rows."""
+    """(address, type, rows, columns, elements from row to row) of a matrix of tensor rows."""
     if not _kinds:
-        import torch
-        _kinds.update({torch.bfloat16: EF_BF16, torch.float16: EF_F16, torch.float32: EF_F32, torch.int8: EF_I8})
+        _load_types()
     kind = _kinds.get(x.dtype)
     if kind is None:
         raise EfError(EF_EINVAL, f"unsupported element type {x.dtype}")
-    if x.dim() != 2:
+    shape = x.shape
+    if len(shape) != 2:
         raise EfError(EF_EINVAL, "a matrix is needed")
-    (rows, cols), (ld, step) = x.shape, x.stride()
+    (rows, cols), (ld, step) = shape, x.stride()
     if cols > 1 and step != 1:
         raise EfError(EF_EINVAL, "a matrix with consecutive row elements is needed")
-    return x.data_ptr(), kind, ld if rows > 1 else max(ld, cols)
+    return x.data_ptr(), kind, rows, cols, ld if rows > 1 or ld > cols else cols
 
 
-def _work(work):
-    return (None, 0) if work is None else (_ptr(work), work.nbytes)
+def _work(work, device):
+    if work is None:
+        return None, 0
+    if work.get_device() != device or not work.is_contiguous():
+        raise EfError(EF_EINVAL, f"scratch must be consecutive memory on device {device}, and is {tuple(work.shape)} on {work.device}")
+    return work.data_ptr(), work.nbytes
 
 
 @functools.lru_cache(maxsize=256)
 def _router(E, k, sigmoid, n_groups, groups_kept, group_best, renorm, scale):
-    return ef_router(E, k, EF_SCORE_SIGMOID if sigmoid else EF_SCORE_SOFTMAX, n_groups, groups_kept, group_best, int(renorm), scale)
+    return bytes(ef_router(E, k, EF_SCORE_SIGMOID if sigmoid else EF_SCORE_SOFTMAX, n_groups, groups_kept, group_best, int(renorm), scale))
+
+
+# an ef_route_operands and an ef_q8_product, made faster than as structures
+_pack_route = struct.Struct("9QQq2i").pack
+_pack_product = struct.Struct("7Q4q9i4x").pack
 
 
 def ef_route_scores_work(T, E, k, n_groups=1, groups_kept=1):
     """Bytes of scratch of ef_route_scores; 0 if a size is out of range."""
-    return int(lib().ef_route_scores_work(C.byref(_router(E, k, False, n_groups, groups_kept, 1, False, 1.0)), T))
+    return int(lib().ef_route_scores_work(_router(E, k, False, n_groups, groups_kept, 1, False, 1.0), T))
 
 
 def ef_route_scores(logits, bias, ids, w, counts, offsets, perm, inv_perm, work, *, sigmoid=False, n_groups=1, groups_kept=1,
                     group_best=1, renorm=False, scale=1.0, stream=None):
     """Routing of logits [T, E]: ids, w [T, k]; counts [E], offsets [E+1], perm, inv_perm [T*k] of the stable grouping."""
-    z, kind, ld = _rows(logits)
-    T, E = logits.shape
-    r = _router(E, ids.shape[1], sigmoid, n_groups, groups_kept, group_best, renorm, scale)
-    wp, wb = _work(work)
-    return _check(None, lib().ef_route_scores(C.byref(r), z, kind, ld, _ptr(bias), T, _ptr(ids), _ptr(w), _ptr(counts), _ptr(offsets),
-                                              _ptr(perm), _ptr(inv_perm), wp, wb, _stream(stream)))
+    z, kind, T, E, ld = _rows(logits)
+    k, on = ids.shape[1], _device(logits, "ef_route_scores")
+    n = T * k
+    r = _router(E, k, sigmoid, n_groups, groups_kept, group_best, renorm, scale)
+    wp, wb = _work(work, on)
+    i32 = _I32
+    rc = lib().ef_route_scores_of(r, _pack_route(
+        z, _vector(bias, _F32, E, on, "bias") or 0, _vector(ids, i32, n, on, "ids") or 0, _vector(w, _F32, n, on, "w") or 0,
+        _vector(counts, i32, E, on, "counts") or 0, _vector(offsets, i32, E + 1, on, "offsets") or 0, _vector(perm, i32, n, on, "perm") or 0,
+        _vector(inv_perm, i32, n, on, "inv_perm") or 0, wp or 0, wb, ld, kind, T), _stream(stream))
+    return _check(None, rc) if rc else rc
 
 
 def ef_quant_rows(x, codes, scales, stream=None):
     """Rows of x [rows, K] to int8 codes [rows, >= K] (zeroed up to the next multiple of 64 columns, of those there are) and scales [rows]."""
-    xp, kind, ldx = _rows(x)
-    cp, ckind, ldc = _rows(codes)
-    if ckind != EF_I8 or codes.shape[0] != x.shape[0] or codes.shape[1] < x.shape[1]:
+    xp, kind, rows, K, ldx = _rows(x)
+    cp, ckind, c_rows, width, ldc = _rows(codes)
+    on = _device(x, "ef_quant_rows")
+    if ckind != EF_I8 or c_rows != rows or width < K:
         raise EfError(EF_EINVAL, "ef_quant_rows: codes must be int8 and as large as x")
-    if scales.numel() < x.shape[0]:
-        raise EfError(EF_EINVAL, "ef_quant_rows: a scale for every row is needed")
-    return _check(None, lib().ef_quant_rows_within(xp, kind, ldx, x.shape[0], x.shape[1], cp, codes.shape[1], ldc, _ptr(scales), _stream(stream)))
+    if codes.get_device() != on:
+        raise EfError(EF_EINVAL, f"ef_quant_rows: x is on {x.device}, codes on {codes.device}")
+    return _check(None, lib().ef_quant_rows_within(xp, kind, ldx, rows, K, cp, width, ldc, _vector(scales, _F32, rows, on, "scales"),
+                                                   _stream(stream)))
 
 
-def _product(a, w, w_scale, out, a_scale, rows, row_div, offsets, swiglu):
-    a_ptr, a_type, lda = _rows(a)
-    out_ptr, out_type, ldo = _rows(out)
+def _product(a, w, w_scale, out, a_scale, rows, row_div, offsets, swiglu, on):
+    """`on`: the device of all operands; None where only their shapes count."""
+    a_ptr, a_type, a_rows, a_cols, lda = _rows(a)
+    out_ptr, out_type, M, cols, ldo = _rows(out)
     shape, strides = w.shape, w.stride()
-    if len(shape) not in (2, 3) or _kinds.get(w.dtype) != EF_I8 or (shape[-1] > 1 and strides[-1] != 1):
+    if len(shape) == 3:
+        (G, N, K), (group, ldw, step) = shape, strides
+    elif len(shape) == 2:
+        (N, K), (ldw, step), G, group = shape, strides, 1, 0
+    if len(shape) not in (2, 3) or _kinds.get(w.dtype) != EF_I8 or (K > 1 and step != 1):
         raise EfError(EF_EINVAL, "ef_matmul_q8: w must be int8 [N, K] or [G, N, K] with consecutive row elements")
-    N, K = shape[-2:]
-    G = shape[0] if len(shape) == 3 else 1
-    a_rows, a_cols = a.shape
-    M, cols = out.shape
     if a_cols < K or (a_type != EF_I8 and a_cols != K):
         raise EfError(EF_EINVAL, f"ef_matmul_q8: rows of {a_cols} against K = {K}")
-    if (cols != (N // 2 if swiglu else N) or w_scale.numel() != G * N or (rows is not None and rows.numel() < M)
-            or (offsets is not None and offsets.numel() != G + 1) or (a_scale is not None and a_scale.numel() < a_rows)):
-        raise EfError(EF_EINVAL, "ef_matmul_q8: out, scales, rows or offsets do not fit the product")
-    return ef_q8_product(a_ptr, _ptr(a_scale), _ptr(rows), _ptr(offsets), w.data_ptr(), _ptr(w_scale), out_ptr, lda,
-                         strides[-2] if N > 1 else (K + 15) // 16 * 16, strides[0] if G > 1 else 0, ldo, a_type, out_type, a_rows, M, N, K,
-                         G, row_div, bool(swiglu))
+    ws, off = _vector(w_scale, _F32, G * N, on, "w_scale") or 0, _vector(offsets, _I32, G + 1, on, "offsets") or 0
+    if cols != (N // 2 if swiglu else N) or w_scale.numel() != G * N or (offsets is not None and offsets.numel() != G + 1):
+        raise EfError(EF_EINVAL, "ef_matmul_q8: out, scales or offsets do not fit the product")
+    if on is not None and (w.get_device() != on or out.get_device() != on):
+        raise EfError(EF_EINVAL, f"ef_matmul_q8: a, w and out are on {a.device}, {w.device} and {out.device}")
+    return _pack_product(a_ptr, _vector(a_scale, _F32, a_rows, on, "a_scale") or 0, _vector(rows, _I32, M, on, "rows") or 0, off,
+                         w.data_ptr(), ws, out_ptr, lda, ldw if N > 1 else (K + 15) // 16 * 16, group if G > 1 else 0, ldo, a_type, out_type, a_rows, M, N, K,
+                         G, row_div, 1 if swiglu else 0)
 
 
 def ef_matmul_q8_work(a, w, w_scale, out, *, a_scale=None, rows=None, row_div=1, offsets=None, swiglu=False):
     """Bytes of scratch of ef_matmul_q8 with the same arguments."""
-    return int(lib().ef_matmul_q8_work(C.byref(_product(a, w, w_scale, out, a_scale, rows, row_div, offsets, swiglu))))
+    return int(lib().ef_matmul_q8_work(_product(a, w, w_scale, out, a_scale, rows, row_div, offsets, swiglu, None)))
 
 
 def ef_matmul_q8(a, w, w_scale, out, work=None, *, a_scale=None, rows=None, row_div=1, offsets=None, swiglu=False, stream=None):
     """out = a_scale * w_scale * (a w^T) with 8-bit codes: `a` [R, K] of codes (with a_scale [R]) or of floats that the call
     quantises, w int8 [N, K] or [G, N, K] with scales [G, N], out [M, N] (swiglu: [M, N/2]).  offsets [G+1]: product rows of
     each matrix; rows [M]: row of `a` (after division by row_div) of each product row."""
-    p = _product(a, w, w_scale, out, a_scale, rows, row_div, offsets, swiglu)
-    wp, wb = _work(work)
-    return _check(None, lib().ef_matmul_q8(C.byref(p), wp, wb, _stream(stream)))
+    on = _device(a, "ef_matmul_q8")
+    p = _product(a, w, w_scale, out, a_scale, rows, row_div, offsets, swiglu, on)
+    wp, wb = _work(work, on)
+    rc = lib().ef_matmul_q8(p, wp, wb, _stream(stream))
+    return _check(None, rc) if rc else rc
 
 
 def ef_combine(y, w, inv_perm, out, stream=None):
     """out[t] = sum_j w[t, j] * y[inv_perm[t*k + j]]; w [T, k] f32, inv_perm [T*k] i32 or None (rows in order)."""
-    yp, ykind, ldy = _rows(y)
-    op, okind, ldo = _rows(out)
-    T, k = w.shape
-    if out.shape[0] != T or out.shape[1] != y.shape[1] or (inv_perm is not None and inv_perm.numel() != T * k):
+    yp, ykind, y_rows, d, ldy = _rows(y)
+    op, okind, T, cols, ldo = _rows(out)
+    tokens, k = w.shape
+    on = _device(out, "ef_combine")
+    inv = _vector(inv_perm, _I32, T * k, on, "inv_perm")
+    if T != tokens or cols != d or (inv_perm is not None and inv_perm.numel() != T * k):
         raise EfError(EF_EINVAL, "ef_combine: shapes do not fit")
-    return _check(None, lib().ef_combine(yp, ykind, ldy, y.shape[0], _ptr(w), _ptr(inv_perm), T, k, y.shape[1], op, okind, ldo,
-                                         _stream(stream)))
+    if y.get_device() != on:
+        raise EfError(EF_EINVAL, f"ef_combine: y is on {y.device}, out on {out.device}")
+    rc = lib().ef_combine(yp, ykind, ldy, y_rows, _vector(w, _F32, T * k, on, "w"), inv, T, k, d, op, okind, ldo, _stream(stream))
+    return _check(None, rc) if rc else rc

@@ -86,6 +86,12 @@ extern "C" int ef_route_scores(const ef_router *r, const void *logits, int type,
     return EF_OK;
 }
 
+extern "C" int ef_route_scores_of(const ef_router *r, const ef_route_operands *o, void *stream) {
+    if (!o) return fail(nullptr, EF_EINVAL, "ef_route_scores: null operands");
+    return ef_route_scores(r, o->logits, o->type, o->ld, o->bias, o->T, o->topk_ids, o->topk_w, o->counts, o->offsets, o->perm, o->inv_perm,
+                           o->work, o->work_bytes, stream);
+}
+
 extern "C" int ef_quant_rows(const void *x, int type, int64_t ldx, int rows, int K, int8_t *codes, int64_t ldc, float *scales,
                              void *stream) {
     return ef_quant_rows_within(x, type, ldx, rows, K, codes, ldc, ldc, scales, stream);
