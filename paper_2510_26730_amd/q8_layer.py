@@ -53,6 +53,10 @@ class Q8Layer:
         T, k = hidden.shape[0], self.k
         if T > self.max_tokens:
             raise ef.EfError(ef.EF_EINVAL, f"Q8Layer: {T} tokens, buffers for {self.max_tokens}")
+        # routing takes its tokens and experts from the logits; the views below have room for hidden's
+        if hidden.shape != (T, self.d) or logits.shape != (T, self.E) or (out is not None and out.shape != (T, self.d)):
+            raise ef.EfError(ef.EF_EINVAL, f"Q8Layer: hidden {tuple(hidden.shape)} and logits {tuple(logits.shape)} (and out, if given) do not fit "
+                                           f"{self.E} experts of {self.d}")
         s = torch.cuda.current_stream(hidden.device) if stream is None else stream
         out = torch.empty(T, self.d, dtype=hidden.dtype, device=hidden.device) if out is None else out
         n = T * k

@@ -199,3 +199,34 @@ def test_operands_in_a_structure_are_checked():
     assert ef.lib().ef_route_scores_of(bytes(ef.ef_router(8, 2, 0, 1, 1, 1, 0, 1.0)), None, None) == ef.EF_EINVAL
     assert ef.lib().ef_route_scores_of(bytes(ef.ef_router(8, 9, 0, 1, 1, 1, 0, 1.0)), bytes(96), None) == ef.EF_EINVAL
     assert "top_k" in ef.ef_last_error(None)
+
+
+# ---- the layer of the operators ------------------------------------------------------------------
+
+@pytest.fixture
+def layer(calls, monkeypatch):
+    """A Q8Layer of 4 experts, d = 64, F = 32, for 6 tokens, whose tensors count as a device's."""
+    from paper_2510_26730_amd.q8_layer import Q8Layer
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda self: 0)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: 4096)
+    made = Q8Layer(torch.zeros(4, 64, 64), torch.zeros(4, 64, 32), 2, 6)
+    calls.made.clear()
+    return made
+
+
+def test_layer_takes_inputs_that_fit(layer, calls):
+    for T in (0, 1, 6):
+        out = layer(torch.zeros(T, 64), torch.zeros(T, 4))
+        assert out.shape == (T, 64) and layer.ids.shape == (T, 2)
+    assert [n for n, _ in calls.made] == ["ef_route_scores_of", "ef_matmul_q8", "ef_matmul_q8", "ef_combine"] * 3
+
+
+@pytest.mark.parametrize("hidden,logits,out", [
+    ((3, 64), (4, 4), None), ((3, 64), (6, 4), None), ((3, 64), (9, 4), None), ((3, 64), (2, 4), None), ((3, 64), (3, 5), None),
+    ((3, 64), (3, 3), None), ((3, 64), (3, 400), None), ((3, 64), (12,), None), ((3, 32), (3, 4), None), ((3, 128), (3, 4), None), ((7, 64), (7, 4), None),
+    ((3, 64), (3, 4), (4, 64)), ((3, 64), (3, 4), (2, 64)), ((3, 64), (3, 4), (3, 32)), ((192,), (3, 4), None)])
+def test_layer_refuses_inputs_that_do_not_fit(layer, calls, hidden, logits, out):
+    """Before its first call: routing more tokens than there are would write behind the buffers' views."""
+    with pytest.raises(ef.EfError):
+        layer(torch.zeros(*hidden), torch.zeros(*logits), None if out is None else torch.zeros(*out))
+    assert not calls.made
