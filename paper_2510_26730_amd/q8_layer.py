@@ -10,6 +10,7 @@ call only enqueues kernels (it may be captured into a graph) and leaves its rout
 from __future__ import annotations
 
 import argparse
+import contextlib
 
 import torch
 
@@ -49,7 +50,8 @@ class Q8Layer:
         self._work = torch.empty(max(work, up, down, 1), dtype=torch.uint8, device=dev)
 
     def __call__(self, hidden, logits, out=None, stream=None):
-        """hidden [T, d], logits [T, E] -> out [T, d] (in hidden's type unless given)."""
+        """hidden [T, d], logits [T, E] -> out [T, d] (in hidden's type unless given).  With `stream`, all of it runs there, on inputs that are
+        ready there, and an out that is not given belongs to that stream."""
         T, k = hidden.shape[0], self.k
         if T > self.max_tokens:
             raise ef.EfError(ef.EF_EINVAL, f"Q8Layer: {T} tokens, buffers for {self.max_tokens}")
@@ -58,7 +60,11 @@ class Q8Layer:
             raise ef.EfError(ef.EF_EINVAL, f"Q8Layer: hidden {tuple(hidden.shape)} and logits {tuple(logits.shape)} (and out, if given) do not fit "
                                            f"{self.E} experts of {self.d}")
         s = torch.cuda.current_stream(hidden.device) if stream is None else stream
-        out = torch.empty(T, self.d, dtype=hidden.dtype, device=hidden.device) if out is None else out
+        if out is None:
+            # on the stream that writes it: memory of another stream's may still be in use there
+            on = contextlib.nullcontext() if stream is None else torch.cuda.stream(torch.cuda.ExternalStream(s, hidden.device) if isinstance(s, int) else s)
+            with on:
+                out = torch.empty(T, self.d, dtype=hidden.dtype, device=hidden.device)
         n = T * k
         self.ids, self.w, self.perm, self.inv_perm = self._ids[:n].view(T, k), self._w[:n].view(T, k), self._perm[:n], self._inv_perm[:n]
         act, y = self._act[:n], self._y[:n]

@@ -51,3 +51,23 @@ def test_combine_without_any_row(y_type, d, pad):
     out[:] = 5
     ef.ef_combine(y[:0, :d], w, inv, out[:3, :d], stream=stream())
     assert out[:3, :d].isnan().all() and (out[:, d:] == 5).all()
+
+
+# ---- the layer -----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_layer_on_a_stream(handle):
+    """The output's memory is of the stream that writes it, and holds what the current stream gives."""
+    from paper_2510_26730_amd.q8_layer import Q8Layer
+    gen = torch.Generator().manual_seed(8)
+    E, d, F, T = 8, 4096, 128, 700
+    layer = Q8Layer(torch.randn(E, 2 * F, d, generator=gen).cuda(), torch.randn(E, d, F, generator=gen).cuda(), 2, T, renorm=True)
+    x, z = torch.randn(T, d, generator=gen).cuda(), torch.randn(T, E, generator=gen).cuda()
+    want = layer(x, z).clone()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    out = layer(x, z, stream=side.cuda_stream if handle else side)
+    side.synchronize()
+    assert torch.equal(out, want)
+    owner = [s["stream"] for s in torch.cuda.memory_snapshot() if s["address"] <= out.data_ptr() < s["address"] + s["total_size"]]
+    assert owner == [side.cuda_stream]

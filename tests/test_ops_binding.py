@@ -230,3 +230,37 @@ def test_layer_refuses_inputs_that_do_not_fit(layer, calls, hidden, logits, out)
     with pytest.raises(ef.EfError):
         layer(torch.zeros(*hidden), torch.zeros(*logits), None if out is None else torch.zeros(*out))
     assert not calls.made
+
+
+@pytest.mark.parametrize("stream", [8192, "object"])
+def test_layer_allocates_where_it_writes(layer, calls, monkeypatch, stream):
+    """The memory of an output belongs to the stream that writes it: allocated on another, it may still be in use there, and be given out again
+    too early."""
+    entered = []
+
+    class On:
+        def __init__(self, s):
+            self.s = s
+
+        def __enter__(self):
+            entered.append(self.s)
+
+        def __exit__(self, *a):
+            entered.pop()
+
+    class Stream:
+        def __init__(self, handle, device=None):
+            self.cuda_stream = handle
+
+    where = []
+    empty = torch.empty
+    monkeypatch.setattr(torch.cuda, "stream", On)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", Stream)
+    monkeypatch.setattr(torch, "empty", lambda *a, **kw: (where.extend(s.cuda_stream for s in entered), empty(*a, **kw))[1])
+    x, z = torch.zeros(3, 64), torch.zeros(3, 4)
+    layer(x, z, stream=stream if stream == 8192 else Stream(8192))
+    assert where == [8192]
+    assert all(args[-1] == 8192 for _, args in calls.made)
+    layer(x, z)
+    layer(x, z, torch.zeros(3, 64), stream=8192)
+    assert where == [8192] and not entered
