@@ -603,7 +603,8 @@ typedef struct ef_router {
  * Comparisons are those of the scores' real values: s and c are formed in 32 bits, and again in 64 where the
  * border of a choice lies within the error of 32.  A logit of -inf or NaN has score 0 and choice value -inf (its
  * expert comes after every other of its token); a bias of NaN counts as -inf; logits of +inf share a softmax
- * evenly.  A token whose scores are all 0 has weights 0, and its ids by the same rules.
+ * evenly.  A token whose scores are all 0 has weights 0, and its ids by the same rules; scores are those of 64 bits, and
+ * renormalised weights have the right quotients also where 32 bits would hold the scores as 0 (a sigmoid of -100).
  *   logits [dev] T rows of E elements of `type` (EF_BF16, EF_F16, EF_F32), ld elements from row to row
  *   topk_ids [T,k] i32, topk_w [T,k] f32, counts [E] i32, offsets [E+1] i32, perm, inv_perm [T*k] i32  [dev]
  * T = 0 is allowed (counts and offsets are zeroed); T*k below 2^31.

@@ -283,6 +283,7 @@ __device__ __forceinline__ float row_min(float x) { return of_bits(row_all(bits_
 __device__ __forceinline__ float row_sum(float x) { return of_bits(row_all(bits_of(x), [](uint32_t p, uint32_t q) { return bits_of(of_bits(p) + of_bits(q)); })); }
 
 constexpr uint32_t kIndexBits = 511;      // low bits of a key: 511 - expert
+constexpr float kDeep = -80.f;            // scores above exp(kDeep) are normal numbers of 32 bits, a softmax's share of 512 too
 
 // Rows of logits (or the bias) come 16 neighbouring lanes after 16 neighbouring quads or elements, go through LDS, and are read
 // back V at a time: a lane that fetched its own V from memory would touch a line of its own with every load, and the address unit
@@ -540,12 +541,19 @@ __global__ __launch_bounds__(64 * NW, VT <= 16 ? 4 : 2) void router_kernel(Route
         const int e = (int)(kIndexBits - (won & kIndexBits));
         int place = 0;
         static_for<1, 16>([&](auto o) { place += dpp<kRor + decltype(o)::value>(l < k ? (uint32_t)e : 1u << 16) < (uint32_t)e; });
-        float w = 0.f;
-        if (mine) {
-            const float z = mine_rows[shape.at(e)];
-            w = !softmax ? 1.f / (1.f + expf(-z)) : z == kMinusInf ? 0.f : z == m ? top : expf(z - m) * top;
-        }
+        const float z = mine ? mine_rows[shape.at(e)] : kMinusInf;
+        const float low = expf(-fabsf(z));
+        float w = softmax ? (z == m ? top : expf(z - m) * top) : (z < 0.f ? low : 1.f) / (1.f + low);
         if (a.r.renorm) {
+            const float depth = softmax ? z - m : z;
+            if (__any(mine && depth < kDeep)) {
+                // Scores that 32 bits do not hold, or in part, keep their quotients without their common factor exp(zc): zc the largest
+                // chosen logit (sigmoid: 0 unless all are negative).  What is 0 in 64 bits counts as 0.
+                const float most = row_max(z), zc = softmax ? most : min_of(most, 0.f);
+                const float x = z == most ? 1.f : expf((softmax ? z : min_of(z, 0.f)) - zc);
+                const bool none = z == kMinusInf || (softmax ? depth < -745.1332f : z <= -709.7827f);
+                w = none ? 0.f : softmax ? x : x / (1.f + low);
+            }
             const float sum = row_sum(w);
             w = sum > 0.f ? w / sum : 0.f;
         }

@@ -5,10 +5,58 @@ import pytest
 import torch
 
 import oracle.ops as ops
+from ops_tolerance import route_weights
 from paper_2510_26730_amd import binding as ef
-from test_gpu_ops import TYPES, f64, stream
+from test_gpu_ops import TYPES, f64, near, run_route, stream
 
 pytestmark = pytest.mark.gpu
+
+
+# ---- routing ------------------------------------------------------------------------------------
+
+def check_weights(z, bias, k, dtype=torch.float32, **kw):
+    got, zd = run_route(z, bias, k, dtype, **kw)
+    want = ops.route_scores(zd, None if bias is None else f64(bias), k, **kw)
+    assert np.array_equal(got["ids"], want["ids"].reshape(-1))
+    tol = route_weights(zd, want["ids"], want["w"], kw.get("sigmoid", False))
+    near(torch.from_numpy(got["w"]).view(-1, k), want["w"], tol, f"weights {tuple(z.shape)} k={k} {kw}")
+
+
+@pytest.mark.parametrize("renorm", [False, True])
+@pytest.mark.parametrize("groups", [dict(), dict(n_groups=4, groups_kept=2, group_best=2)])
+@pytest.mark.parametrize("with_bias", [False, True])
+@pytest.mark.parametrize("low", [-60, -86, -90, -120, -200, -600])
+def test_weights_of_very_low_sigmoid_scores(low, with_bias, groups, renorm):
+    """Scores that 32 bits cannot hold still have the right quotients; rows whose chosen ones straddle the border of 32 bits."""
+    gen = torch.Generator().manual_seed(-low)
+    z = low + 4 * torch.rand(60, 64, generator=gen)
+    z[:20] = low + 4 * torch.randint(0, 200, (20, 64), generator=gen).float() / 100
+    z[20:40, 5] = torch.linspace(low, 3, 20)
+    bias = torch.linspace(0, 1, 64)[torch.randperm(64, generator=gen)] if with_bias else None
+    check_weights(z, bias, 4, sigmoid=True, renorm=renorm, scale=2.5, **groups)
+
+
+@pytest.mark.parametrize("renorm", [False, True])
+@pytest.mark.parametrize("best", [1, 2])
+@pytest.mark.parametrize("depth", [20, 90, 105, 130, 600])
+def test_weights_of_experts_far_below_the_top(depth, best, renorm):
+    """A softmax whose bias chooses experts `depth` below the largest logit."""
+    gen = torch.Generator().manual_seed(depth)
+    z = 3 * torch.rand(50, 32, generator=gen)
+    z[:, 8:24] -= depth
+    bias = torch.zeros(32)
+    bias[8:24] = 3 + torch.linspace(0, 1, 16)[torch.randperm(16, generator=gen)]
+    check_weights(z, bias, 4, renorm=renorm)
+    check_weights(z, bias, 4, renorm=renorm, n_groups=4, groups_kept=2, group_best=best)
+
+
+def test_chosen_scores_that_are_all_0():
+    """Behind a logit of +inf a softmax leaves nothing for the others, whatever the bias chooses."""
+    z = torch.randn(8, 16, generator=torch.Generator().manual_seed(2))
+    z[:, 3] = float("inf")
+    bias = torch.linspace(2, 3, 16)
+    bias[3] = 0
+    check_weights(z, bias, 4, renorm=True)
 
 
 # ---- rows to 8 bits ------------------------------------------------------------------------------
