@@ -487,7 +487,9 @@ __global__ __launch_bounds__(64 * NW, VT <= 16 ? 4 : 2) void router_kernel(Route
             kept = rank < a.r.groups_kept;
             if (a.r.groups_kept < a.r.n_groups && margin >= 0.f) {
                 const float worst = row_min(kept ? value : __builtin_inff()), best = row_max(kept ? kMinusInf : value);
-                near = worst - best <= margin;
+                // a sum of two that passes 32 bits: the wave's tokens are decided in 64
+                const float inf = __builtin_inff();
+                near = worst - best <= margin || __any(fabsf(value) == inf && fabsf(b1) < inf && fabsf(b2) < inf);
             }
         }
         uint32_t key[VT];

@@ -59,6 +59,17 @@ def test_chosen_scores_that_are_all_0():
     check_weights(z, bias, 4, renorm=True)
 
 
+def test_sums_of_two_best_beyond_32_bits():
+    z = torch.randn(40, 16, generator=torch.Generator().manual_seed(9))
+    bias = torch.tensor([3.0e38, 3.0e38, 0, 0, 3.1e38, 3.1e38, 0, 0, 3.3e38, 2.7e38, 0, 0, 3.2e38, 3.2e38, 0, 0])
+    for kept in (1, 2, 3):
+        check_weights(z, bias, 2, sigmoid=True, n_groups=4, groups_kept=kept, group_best=2)
+        check_weights(z, -bias, 2, n_groups=4, groups_kept=kept, group_best=2)
+        check_weights(z[:, :8], bias[[0, 1, 4, 5, 8, 9, 12, 13]], 2, sigmoid=True, n_groups=4, groups_kept=kept, group_best=2)
+        check_weights(z[:, :8], -bias[[0, 1, 4, 5, 8, 9, 12, 13]], 2, sigmoid=True, n_groups=4, groups_kept=kept, group_best=2)
+        check_weights(z[:, :8], -bias[[12, 13, 4, 5, 8, 9, 0, 1]], 2, n_groups=4, groups_kept=kept, group_best=2)
+
+
 # ---- rows to 8 bits ------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
