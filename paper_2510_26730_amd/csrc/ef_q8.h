@@ -145,6 +145,19 @@ __device__ __forceinline__ Q8Row q8_row(const Q8Args &p, int i) {
     return Q8Row{r, p.a_scale ? p.a_scale[r] : 0.f};
 }
 
+// silu(g) * u.  silu_mul() gives 0 below a gate of -87.3, where the quotient is still a number of 32 bits (and, times a large u, not a small
+// one): there it is g exp(g), which differs by exp(g); exp(-64) is taken out of the exponential.
+constexpr float kDeepGate = -87.f;
+__device__ __forceinline__ float q8_silu_mul_deep(float g, float u) {
+    return g < kDeepGate ? g * __expf(g + 64.f) * u * 0x1.969d47321e4ccp-93f : silu_mul(g, u);
+}
+// v = silu(v) * u
+__device__ __forceinline__ void q8_silu_mul4(float (&v)[4], const float (&u)[4]) {
+    const bool deep = __any(fminf(fminf(v[0], v[1]), fminf(v[2], v[3])) < kDeepGate);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = deep ? q8_silu_mul_deep(v[e], u[e]) : silu_mul(v[e], u[e]);
+}
+
 // Four loads of a wave take 16 rows x 256 bytes, a step: lane 16g + 4q + c gets chunk c (16 bytes) of segment g (64 bytes) of row
 // 4q + j in load j.  Neighbouring lanes have to be neighbours in memory: four lanes in one segment are one cycle of a compute unit's
 // address unit, in four rows they are four (16 bytes a clock, less than the products need).  The matrix instruction wants rows in the

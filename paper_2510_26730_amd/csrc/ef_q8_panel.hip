@@ -166,12 +166,13 @@ __global__ __launch_bounds__(256 * KS) void q8_panel_kernel(Q8Args p, int npanel
             if (row >= t.row_end) continue;
 #pragma unroll
             for (int b = 0; b < (PAIR ? RA / 2 : RA); ++b) {
-                float v[4];
+                float v[4], up[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     v[e] = (float)acc[b][j][e] * xs * sc[16 * b + e];
-                    if constexpr (PAIR) v[e] = silu_mul(v[e], (float)acc[b + RA / 2][j][e] * xs * sc[16 * (b + RA / 2) + e]);
+                    if constexpr (PAIR) up[e] = (float)acc[b + RA / 2][j][e] * xs * sc[16 * (b + RA / 2) + e];
                 }
+                if constexpr (PAIR) q8_silu_mul4(v, up);
                 q8_store4<decltype(TYPE)::value>(p, row, col0 + 16 * b + 4 * g, n_end, v);
             }
         }

@@ -5,9 +5,9 @@ import pytest
 import torch
 
 import oracle.ops as ops
-from ops_tolerance import route_weights
+from ops_tolerance import U, route_weights
 from paper_2510_26730_amd import binding as ef
-from test_gpu_ops import TYPES, f64, near, run_route, stream
+from test_gpu_ops import TYPES, f64, near, run_route, stream, weights
 
 pytestmark = pytest.mark.gpu
 
@@ -89,6 +89,40 @@ def test_codes_in_columns_of_a_wider_matrix(rows, K, first, last, pitch, dtype):
     assert np.array_equal(wide[:, first:first + K].cpu().numpy(), q) and np.array_equal(f64(scales), s)
     assert (wide[:, first + K:first + padded] == 0).all()
     assert (wide[:, :first] == 99).all() and (wide[:, first + padded:] == 99).all() and (room[rows * pitch:] == 99).all()
+
+
+# ---- products ------------------------------------------------------------------------------------
+
+# every form: rows, K, N (swiglu: twice the columns), rows of each group
+SHAPES = [(2, 512, 256, None), (12, 512, 256, None), (30, 320, 512, None), (200, 192, 2048, None), (100, 1300, 8300, None), (520, 192, 2300, None),
+          (520, 1152, 14000, None), (0, 1088, 1408, [30, 0, 1, 64, 65, 7] * 9), (0, 320, 512, [90, 0, 129, 33])]
+IDS = [f"{s[0]}-{s[1]}-{s[2]}" for s in SHAPES]
+
+
+@pytest.mark.parametrize("M,K,N,counts", SHAPES, ids=IDS)
+def test_swiglu_of_gates_whose_exponential_passes_32_bits(M, K, N, counts):
+    """silu(g) is a 32-bit number down to g = -91, and its product with a large u farther down.  Gates from -102 to -60 and from 60 to 102."""
+    gen = torch.Generator().manual_seed(M + N)
+    M, G = sum(counts) if counts else M, len(counts) if counts else 1
+    x = torch.linspace(0.6, 1.02, M)[torch.randperm(M, generator=gen)][:, None].expand(M, K).contiguous()
+    w, ws = weights(gen, G, N, K)
+    F = N // 2
+    w[:, :F], w[:, F:] = -100, 90
+    w[:, 1:F:5] = 100
+    ws[:, :F] = 1 / K
+    ws[:, F:] = torch.logspace(8, 12, F, device="cuda") / K
+    off = None if counts is None else np.concatenate([[0], np.cumsum(counts)])
+    out = torch.empty(M, F, device="cuda")
+    a, xc, kw = w if counts else w[0], x.cuda(), dict(swiglu=True, offsets=None if off is None else torch.tensor(off, dtype=torch.int32, device="cuda"))
+    work = torch.empty(ef.ef_matmul_q8_work(xc, a, ws, out, **kw), dtype=torch.uint8, device="cuda")
+    ef.ef_matmul_q8(xc, a, ws, out, work, stream=stream(), **kw)
+    q, s = ops.quant_rows(f64(x))
+    y = ops.matmul_q8(q, s, w.cpu().numpy(), f64(ws), offsets=off)
+    want = ops.matmul_q8(q, s, w.cpu().numpy(), f64(ws), offsets=off, swiglu=True)
+    # three roundings in front of each factor, which silu multiplies by up to 1 + |g|; the exponential's argument and itself; subnormal results
+    tol = np.abs(want) * (8 * np.abs(y[:, :F]) + 24) * U + 2.0 ** -126
+    near(out, want, tol, f"swiglu M={M} N={N} K={K} G={G}")
+    assert (np.abs(want) > 1e-34).all()
 
 
 # ---- weighted sum --------------------------------------------------------------------------------
