@@ -650,8 +650,9 @@ int ef_quant_rows_within(const void *x, int type, int64_t ldx, int rows, int K, 
  *   y[i][n] = a_scale[r] * w_scale[g][n] * sum_k a[r][k] * w[g][n][k],
  * g the group of product row i (offsets[g] <= i < offsets[g+1]), r = rows[i] / row_div its row of `a`
  * (rows == NULL: r = i).  The sum is in whole numbers and exact.  With swiglu the rows of a matrix are F gate rows
- * and then F up rows (N = 2F), and out[i][f] = silu(y[i][f]) * y[i][F+f]; otherwise out = y.  Rounded once, to out_type.
- * Values beyond EF_F16's range become infinite.
+ * and then F up rows (N = 2F), and out[i][f] = silu(y[i][f]) * y[i][F+f]; otherwise out = y.  y is formed in 32 bits: the sum
+ * rounds once, and so does each of the two factors (three half steps); out rounds to out_type.  Nothing on the way overflows
+ * where y does not.  Values beyond EF_F16's range become infinite.
  * `a` of 16 or 32 bits is quantised in the call as ef_quant_rows does (all a_rows rows, once).
  * Rows outside all groups are not written.  Offsets outside 0..M or descending, and row numbers outside `a`, are
  * caught on the device: an offset is clamped (one that lies before an earlier one counts as that one), a row of `a`

@@ -145,6 +145,14 @@ __device__ __forceinline__ Q8Row q8_row(const Q8Args &p, int i) {
     return Q8Row{r, p.a_scale ? p.a_scale[r] : 0.f};
 }
 
+// The scales on a sum.  Sum times row scale passes 32 bits from a row scale of 2^97 on (values from 2e31), though the channel's scale may bring
+// the result back, so a row scale of 2^64 and more gives 2^32 away, which the result gets back at its end: in between there is
+// neither an overflow nor a subnormal number that the result has not.
+constexpr float kLargeScale = 0x1p64f;
+struct Q8Scale { float s, back; };
+__device__ __forceinline__ Q8Scale q8_scale(float s) { return s >= kLargeScale ? Q8Scale{s * 0x1p-32f, 0x1p32f} : Q8Scale{s, 1.f}; }
+__device__ __forceinline__ float q8_value(int sum, Q8Scale row, float channel) { return (float)sum * row.s * channel * row.back; }
+
 // silu(g) * u.  silu_mul() gives 0 below a gate of -87.3, where the quotient is still a number of 32 bits (and, times a large u, not a small
 // one): there it is g exp(g), which differs by exp(g); exp(-64) is taken out of the exponential.
 constexpr float kDeepGate = -87.f;

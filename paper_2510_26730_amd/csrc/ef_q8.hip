@@ -378,11 +378,12 @@ __global__ __launch_bounds__(64 * (KS > 4 ? KS : 4)) void q8_stream_kernel(Q8Arg
         for (int j = 0; j < TT; ++j) {
             const int row = t.row0 + 16 * j + i;
             if (row >= t.row_end) continue;
+            const Q8Scale scale = q8_scale(xs[j]);
             float v[NB][4];
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[b][e] = (float)acc[b][j][e] * xs[j] * ws[b][e];
+                for (int e = 0; e < 4; ++e) v[b][e] = q8_value(acc[b][j][e], scale, ws[b][e]);
             if constexpr (PAIR) q8_silu_mul4(v[0], v[1]);
 #pragma unroll
             for (int b = 0; b < (PAIR ? 1 : NB); ++b) q8_store4<decltype(TYPE)::value>(p, row, n0 + 16 * b + 4 * g, n_end, v[b]);

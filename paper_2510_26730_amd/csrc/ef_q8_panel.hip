@@ -162,15 +162,15 @@ __global__ __launch_bounds__(256 * KS) void q8_panel_kernel(Q8Args p, int npanel
 #pragma unroll
         for (int j = 0; j < kOwn; ++j) {
             const int tile = team * kOwn + j, row = t.row0 + 16 * tile + i;
-            const float xs = xscale[16 * tile + i];
+            const Q8Scale xs = q8_scale(xscale[16 * tile + i]);
             if (row >= t.row_end) continue;
 #pragma unroll
             for (int b = 0; b < (PAIR ? RA / 2 : RA); ++b) {
                 float v[4], up[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    v[e] = (float)acc[b][j][e] * xs * sc[16 * b + e];
-                    if constexpr (PAIR) up[e] = (float)acc[b + RA / 2][j][e] * xs * sc[16 * (b + RA / 2) + e];
+                    v[e] = q8_value(acc[b][j][e], xs, sc[16 * b + e]);
+                    if constexpr (PAIR) up[e] = q8_value(acc[b + RA / 2][j][e], xs, sc[16 * (b + RA / 2) + e]);
                 }
                 if constexpr (PAIR) q8_silu_mul4(v, up);
                 q8_store4<decltype(TYPE)::value>(p, row, col0 + 16 * b + 4 * g, n_end, v);

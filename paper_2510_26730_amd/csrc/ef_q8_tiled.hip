@@ -168,8 +168,10 @@ __global__ __launch_bounds__(256, RA *RB >= 16 ? 1 : 2) void q8_tiled_kernel(Q8A
         }
     char *mine = lds + wave * (kStages * kStageBytes / 4);
     static_assert(32 * (kCols * 4 + 16) <= kStages * kStageBytes / 4, "a tile of results fits a wave's share of the ring");
-    const auto leave = [&](auto TYPE, auto DEEP) {
-        float lowest = 0.f;
+    // Returns whether a result needs CAREFUL, the forms for gates and row scales that the plain ones are not right for
+    const auto leave = [&](auto TYPE, auto CAREFUL) {
+        constexpr bool careful = decltype(CAREFUL)::value;
+        float lowest = 0.f, largest = 0.f;
         constexpr int type = decltype(TYPE)::value, size = type == EF_F32 ? 4 : 2, pitch = kCols * size + 16;
         constexpr int kPieces = kCols * size / 16, kTurns = 32 * kPieces / 64;    // 16-byte pieces of a row; of a tile, for each lane
         const bool whole = ((reinterpret_cast<size_t>(p.out) | (size_t)p.ldo * size) & 15) == 0 && (col0 * size & 15) == 0 && col0 + kCols <= n_end;
@@ -178,6 +180,8 @@ __global__ __launch_bounds__(256, RA *RB >= 16 ? 1 : 2) void q8_tiled_kernel(Q8A
             const int row0 = t.row0 + (wt * RB + y) * 32;
             if (row0 >= t.row_end) break;
             const float xs = xscale[(wt * RB + y) * 32 + i];
+            largest = fmaxf(largest, xs);
+            const auto value = [&](int sum, float channel) { return careful ? q8_value(sum, q8_scale(xs), channel) : (float)sum * xs * channel; };
 #pragma unroll
             for (int x = 0; x < RA; x += PAIR ? 2 : 1)
 #pragma unroll
@@ -185,11 +189,11 @@ __global__ __launch_bounds__(256, RA *RB >= 16 ? 1 : 2) void q8_tiled_kernel(Q8A
                     float v[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        v[e] = (float)acc[x][y][4 * q + e] * xs * sc[x][4 * q + e];
+                        v[e] = value(acc[x][y][4 * q + e], sc[x][4 * q + e]);
                         if constexpr (PAIR) {
-                            const float u = (float)acc[x + 1][y][4 * q + e] * xs * sc[x + 1][4 * q + e];
+                            const float u = value(acc[x + 1][y][4 * q + e], sc[x + 1][4 * q + e]);
                             lowest = fminf(lowest, v[e]);
-                            v[e] = decltype(DEEP)::value ? q8_silu_mul_deep(v[e], u) : silu_mul(v[e], u);
+                            v[e] = careful ? q8_silu_mul_deep(v[e], u) : silu_mul(v[e], u);
                         }
                     }
                     q8_put4<type>(mine + i * pitch, (PAIR ? x / 2 : x) * 32 + 8 * q + 4 * g, v);
@@ -224,12 +228,11 @@ __global__ __launch_bounds__(256, RA *RB >= 16 ? 1 : 2) void q8_tiled_kernel(Q8A
             }
             wave_lds_sync();
         }
-        return lowest;
+        return largest >= kLargeScale || lowest < kDeepGate;
     };
+    // once more where needed; a branch for every four gates or a third factor on every sum cost the large products up to 3 %
     q8_by_type(p.out_type, [&](auto TYPE) {
-        const float lowest = leave(TYPE, std::false_type{});
-        if constexpr (PAIR)      // once more, with such gates; a branch for every four elements cost the large products 3 %
-            if (__any(lowest < kDeepGate)) leave(TYPE, std::true_type{});
+        if (__any(leave(TYPE, std::false_type{}))) leave(TYPE, std::true_type{});
     });
 }
 

@@ -7,7 +7,7 @@ import torch
 import oracle.ops as ops
 from ops_tolerance import U, route_weights
 from paper_2510_26730_amd import binding as ef
-from test_gpu_ops import TYPES, f64, near, run_route, stream, weights
+from test_gpu_ops import TYPES, check_product, f64, near, run_route, stream, weights
 
 pytestmark = pytest.mark.gpu
 
@@ -123,6 +123,40 @@ def test_swiglu_of_gates_whose_exponential_passes_32_bits(M, K, N, counts):
     tol = np.abs(want) * (8 * np.abs(y[:, :F]) + 24) * U + 2.0 ** -126
     near(out, want, tol, f"swiglu M={M} N={N} K={K} G={G}")
     assert (np.abs(want) > 1e-34).all()
+
+
+@pytest.mark.parametrize("swiglu", [False, True])
+@pytest.mark.parametrize("M,K,N,counts", SHAPES, ids=IDS)
+def test_products_whose_sum_and_scale_pass_32_bits(M, K, N, counts, swiglu):
+    """Rows near the type's largest value beside ordinary ones: a sum times the row's scale is beyond 32 bits, their result is not."""
+    gen = torch.Generator().manual_seed(K + N)
+    M = sum(counts) if counts else M
+    x = torch.rand(M, K, generator=gen)
+    x[::3] *= 1e38
+    check_product(gen, x, len(counts) if counts else 1, N, counts, swiglu=swiglu, out="f32", magnitude=1e-37 if swiglu else 1e-6)
+
+
+@pytest.mark.parametrize("M,K,N,counts", SHAPES, ids=IDS)
+def test_large_scales_of_sums_that_are_0(M, K, N, counts):
+    """0 times two scales whose product is beyond 32 bits is 0, a sum of more is infinite, and neither touches the rows beside."""
+    gen = torch.Generator().manual_seed(K)
+    M = sum(counts) if counts else M
+    G = len(counts) if counts else 1
+    x = torch.rand(M, K, generator=gen) + 0.5
+    x[::2] *= 2.0 ** 110
+    w, ws = weights(gen, G, N, K)
+    w[:, ::2] = 0
+    w[:, 1::2] = 1
+    w[:, 1::4] = -1
+    ws[:] = 2.0 ** 110
+    off = None if counts is None else torch.tensor(np.concatenate([[0], np.cumsum(counts)]), dtype=torch.int32, device="cuda")
+    out = torch.empty(M, N, device="cuda")
+    a, xc = w if counts else w[0], x.cuda()
+    work = torch.empty(ef.ef_matmul_q8_work(xc, a, ws, out, offsets=off), dtype=torch.uint8, device="cuda")
+    ef.ef_matmul_q8(xc, a, ws, out, work, offsets=off, stream=stream())
+    assert (out[:, ::2] == 0).all()
+    assert (out[::2, 1::4] == -float("inf")).all() and (out[::2, 3::4] == float("inf")).all()
+    assert out[1::2, 1::2].isfinite().all() and (out[1::2, 1::2] != 0).all()
 
 
 # ---- weighted sum --------------------------------------------------------------------------------
