@@ -22,13 +22,14 @@ namespace {
 // ------------------------------------------------------------------------------------------------
 
 // the whole number nearest x / s, ties to even, |x| / s <= 127.5.  The product with the reciprocal finds it to within one; the
-// residual x - q s, which a multiply-add gives exactly here, says on which side of the halves x / s lies.
+// residual x - q s, which a multiply-add gives exactly here, says on which side of the halves x / s lies; twice it against s, since s / 2 need
+// not be a number of 32 bits (s below 2^-125).
 __device__ __forceinline__ int quant_code(float x, float s, float inv) {
     float q = __builtin_rintf(x * inv);
-    const float r = __builtin_fmaf(-q, s, x), h = 0.5f * s;
+    const float r = 2.f * __builtin_fmaf(-q, s, x);
     const bool odd = (int)q & 1;
-    if (r > h || (r == h && odd)) q += 1.f;
-    else if (r < -h || (r == -h && odd)) q -= 1.f;
+    if (r > s || (r == s && odd)) q += 1.f;
+    else if (r < -s || (r == -s && odd)) q -= 1.f;
     return (int)q;
 }
 
@@ -78,7 +79,7 @@ __device__ __forceinline__ uint32_t quant_four(const float *v, float s, float in
         off = fmaxf(off, fabsf(__builtin_fmaf(12582912.f - sum, s, v[i])));
         y[i] = __builtin_bit_cast(uint32_t, sum);
     }
-    if (off >= 0.5f * s) {
+    if (off >= 0.5f * s) {      // (an s / 2 that has to round separates the same residuals)
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] = (uint32_t)quant_code(v[i], s, inv);
     }

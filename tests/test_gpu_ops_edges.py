@@ -7,7 +7,7 @@ import torch
 import oracle.ops as ops
 from ops_tolerance import U, route_weights
 from paper_2510_26730_amd import binding as ef
-from test_gpu_ops import TYPES, check_product, f64, near, run_route, stream, weights
+from test_gpu_ops import TYPES, check_product, check_quant, f64, near, run_route, stream, weights
 
 pytestmark = pytest.mark.gpu
 
@@ -89,6 +89,21 @@ def test_codes_in_columns_of_a_wider_matrix(rows, K, first, last, pitch, dtype):
     assert np.array_equal(wide[:, first:first + K].cpu().numpy(), q) and np.array_equal(f64(scales), s)
     assert (wide[:, first + K:first + padded] == 0).all()
     assert (wide[:, :first] == 99).all() and (wide[:, first + padded:] == 99).all() and (room[rows * pitch:] == 99).all()
+
+
+def test_quant_rows_at_halves_of_the_smallest_scales():
+    """Scales between 2^-126 and 2^-125, whose halves are no 32-bit numbers: the values on both sides of them."""
+    rng = np.random.default_rng(4)
+    most = (127 * 2.0 ** -126 * (1 + rng.random(400))).astype(np.float32)
+    scale = np.maximum((most.astype(np.float64) / 127).astype(np.float32), np.float32(2.0 ** -126)).astype(np.float64)
+    x = np.zeros((400, 64), np.float32)
+    x[:, 0] = most
+    for c in range(1, 64):
+        half = (c // 4 + 0.5) * scale * (1 if c % 2 else -1)
+        x[:, c] = half.astype(np.float32)
+        x[:, c] = np.nextafter(x[:, c], np.float32(np.inf if c % 4 < 2 else -np.inf))
+    check_quant(torch.from_numpy(x))
+    check_quant(torch.from_numpy(x[:, :63].copy()))
 
 
 # ---- products ------------------------------------------------------------------------------------
