@@ -607,7 +607,7 @@ typedef struct ef_router {
  * renormalised weights have the right quotients also where 32 bits would hold the scores as 0 (a sigmoid of -100).
  *   logits [dev] T rows of E elements of `type` (EF_BF16, EF_F16, EF_F32), ld elements from row to row
  *   topk_ids [T,k] i32, topk_w [T,k] f32, counts [E] i32, offsets [E+1] i32, perm, inv_perm [T*k] i32  [dev]
- * T = 0 is allowed (counts and offsets are zeroed); T*k below 2^31.
+ * T = 0 is allowed (counts and offsets are zeroed); T*k below 2^31, T at most 2^29 - 64.
  */
 size_t ef_route_scores_work(const ef_router *r, int T);   /* enough for fewer tokens too; 0 if r or T is out of range */
 int ef_route_scores(const ef_router *r, const void *logits, int type, int64_t ld, const float *bias, int T,

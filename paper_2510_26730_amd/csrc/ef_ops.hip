@@ -31,7 +31,8 @@ const char *router_fault(const ef_router *r) {
     if (r->renorm != 0 && r->renorm != 1) return "renorm must be 0 or 1";
     return nullptr;
 }
-bool router_tokens_ok(const ef_router *r, int T) { return T >= 0 && (long long)T * r->top_k <= 0x7FFFFFFFll; }
+// a launch has fewer than 2^32 lanes: eight for a token at most
+bool router_tokens_ok(const ef_router *r, int T) { return T >= 0 && T <= (1 << 29) - 64 && (long long)T * r->top_k <= 0x7FFFFFFFll; }
 
 int router_tiles(const ef_router *r, int T) {
     const int tile = ef::router_tile(*r, T);

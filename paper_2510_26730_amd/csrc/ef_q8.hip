@@ -510,7 +510,21 @@ hipError_t launch_quant(const QuantArgs &a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_quant_rows(const QuantArgs &a, hipStream_t s) {
+// A launch has fewer than 2^32 lanes, and some forms take 256 for a row
+constexpr int kRowsPerLaunch = 1 << 23;
+
+hipError_t launch_quant_rows(const QuantArgs &all, hipStream_t s) {
+    QuantArgs a = all;
+    for (; a.rows > kRowsPerLaunch;) {
+        QuantArgs part = a;
+        part.rows = kRowsPerLaunch;
+        const hipError_t e = launch_quant_rows(part, s);
+        if (e != hipSuccess) return e;
+        a.x = static_cast<const char *>(a.x) + kRowsPerLaunch * a.ldx * (a.type == EF_F32 ? 4 : a.type == EF_I8 ? 1 : 2);
+        a.codes += kRowsPerLaunch * a.ldc;
+        if (a.scales) a.scales += kRowsPerLaunch;
+        a.rows -= kRowsPerLaunch;
+    }
     if (a.rows <= 0) return hipSuccess;
     switch (a.type) {
         case EF_I8: hipLaunchKernelGGL(pad_rows_kernel, dim3(a.rows), dim3(256), 0, s, a); return hipGetLastError();
@@ -566,7 +580,23 @@ hipError_t launch_q8_product(const Q8Args &p, hipStream_t s) {
     return launch_q8_tiled(p, (long long)per * p.K >= 512 * 1024 && tiles * panels(p.swiglu ? 128 : 256) >= 160, s);
 }
 
-hipError_t launch_combine_rows(const CombineArgs &a, hipStream_t s) {
+hipError_t launch_combine_rows(const CombineArgs &all, hipStream_t s) {
+    CombineArgs a = all;
+    for (; a.T > kRowsPerLaunch;) {
+        CombineArgs part = a;
+        part.T = kRowsPerLaunch;
+        const hipError_t e = launch_combine_rows(part, s);
+        if (e != hipSuccess) return e;
+        const long long slots = (long long)kRowsPerLaunch * a.k;
+        if (a.inv_perm) a.inv_perm += slots;
+        else {
+            a.y = static_cast<const char *>(a.y) + slots * a.ldy * (a.y_type == EF_F32 ? 4 : 2);
+            a.y_rows -= (int)slots;
+        }
+        a.w += slots;
+        a.out = static_cast<char *>(a.out) + kRowsPerLaunch * a.ldo * (a.out_type == EF_F32 ? 4 : 2);
+        a.T -= kRowsPerLaunch;
+    }
     if (a.T <= 0) return hipSuccess;
     return a.y_type == EF_BF16 ? launch_combine_y<EF_BF16>(a, s) : a.y_type == EF_F16 ? launch_combine_y<EF_F16>(a, s)
                                                                                       : launch_combine_y<EF_F32>(a, s);

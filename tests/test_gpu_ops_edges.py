@@ -7,7 +7,7 @@ import torch
 import oracle.ops as ops
 from ops_tolerance import U, route_weights
 from paper_2510_26730_amd import binding as ef
-from test_gpu_ops import TYPES, check_product, check_quant, f64, near, run_route, stream, weights
+from test_gpu_ops import TYPES, check_product, check_quant, f64, near, product_tolerance, run_route, stream, weights
 
 pytestmark = pytest.mark.gpu
 
@@ -106,6 +106,27 @@ def test_quant_rows_at_halves_of_the_smallest_scales():
     check_quant(torch.from_numpy(x[:, :63].copy()))
 
 
+def test_more_rows_than_a_launch_has_workgroups():
+    """2^24 workgroups of 256 lanes are more than one launch takes."""
+    n, K = (1 << 24) + 3, 3
+    base = torch.randn(1000, K, generator=torch.Generator().manual_seed(1)).bfloat16().cuda()
+    at = torch.arange(n, device="cuda") % 1000
+    x, codes, scales = base[at], torch.full((n, K), 99, dtype=torch.int8, device="cuda"), torch.full((n,), -1.0, device="cuda")
+    ef.ef_quant_rows(x, codes, scales, stream=stream())
+    q, s = ops.quant_rows(f64(base))
+    q, s = torch.from_numpy(q).to(torch.int8).cuda(), torch.from_numpy(s).float().cuda()
+    assert torch.equal(codes, q[at]) and torch.equal(scales, s[at])
+    w, ws = weights(torch.Generator().manual_seed(2), 1, 5, K)
+    rows = torch.tensor([0, n - 1, n, 1 << 24, 1234567], dtype=torch.int32, device="cuda")
+    want = ops.matmul_q8(q[at[rows.long().clamp(max=n - 1)]].cpu().numpy(), f64(s[at[rows.long().clamp(max=n - 1)]]), w.cpu().numpy(), f64(ws))
+    want[2] = np.nan
+    for a, kw in ((x, {}), (codes, dict(a_scale=scales))):
+        out = torch.empty(5, 5, device="cuda")
+        work = torch.empty(ef.ef_matmul_q8_work(a, w[0], ws, out, rows=rows, **kw), dtype=torch.uint8, device="cuda")
+        ef.ef_matmul_q8(a, w[0], ws, out, work, rows=rows, stream=stream(), **kw)
+        near(out, want, product_tolerance(want, torch.float32), f"a row of {n}")
+
+
 # ---- products ------------------------------------------------------------------------------------
 
 # every form: rows, K, N (swiglu: twice the columns), rows of each group
@@ -193,6 +214,16 @@ def test_combine_without_any_row(y_type, d, pad):
     out[:] = 5
     ef.ef_combine(y[:0, :d], w, inv, out[:3, :d], stream=stream())
     assert out[:3, :d].isnan().all() and (out[:, d:] == 5).all()
+
+
+def test_combine_of_more_tokens_than_a_launch_has_workgroups():
+    n = (1 << 24) + 3
+    y, w, out = torch.randn(n, 1, device="cuda"), torch.randn(n, 1, device="cuda"), torch.full((n, 1), 7.0, device="cuda")
+    ef.ef_combine(y, w, None, out, stream=stream())
+    assert torch.equal(out, y * w)
+    inv = torch.arange(n - 1, -1, -1, dtype=torch.int32, device="cuda")
+    ef.ef_combine(y, w, inv, out, stream=stream())
+    assert torch.equal(out, y.flip(0) * w)
 
 
 # ---- the layer -----------------------------------------------------------------------------------

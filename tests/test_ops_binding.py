@@ -68,6 +68,11 @@ def test_width_is_checked():
         assert refuse(width, ldc) == ef.EF_EINVAL and "width" in ef.ef_last_error(None)
 
 
+def test_tokens_of_a_launch_are_checked():
+    for k, most in ((1, (1 << 29) - 64), (4, (1 << 29) - 64), (8, (1 << 28) - 1)):
+        assert ef.ef_route_scores_work(most, 16, k) > 0 and ef.ef_route_scores_work(most + 1, 16, k) == 0
+
+
 class Other(torch.Tensor):
     def get_device(self):
         return 1
