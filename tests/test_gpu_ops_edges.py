@@ -59,6 +59,25 @@ def test_chosen_scores_that_are_all_0():
     check_weights(z, bias, 4, renorm=True)
 
 
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("with_bias", [False, True])
+@pytest.mark.parametrize("groups", [dict(), dict(n_groups=4, groups_kept=2, group_best=2), dict(n_groups=4, groups_kept=2)])
+def test_weights_beside_masked_logits(sigmoid, dtype, with_bias, groups):
+    """-inf, NaN, +inf and the type's lowest value in some rows say nothing about how far the weights of others may be off."""
+    gen = torch.Generator().manual_seed(11)
+    z = torch.randn(60, 48, generator=gen)
+    inf, nan, low = float("inf"), float("nan"), torch.finfo(TYPES[dtype]).min
+    z[0], z[1], z[2] = -inf, nan, low
+    z[3, ::2], z[4, :46], z[5, 7], z[6, 3:9] = nan, -inf, inf, inf
+    z[7, ::3] = low
+    z[8, 1:] = low
+    z[10:30][torch.rand(20, 48, generator=gen) < 0.9] = -inf
+    z[30:40][torch.rand(10, 48, generator=gen) < 0.9] = low
+    bias = 0.3 * torch.randn(48, generator=gen) if with_bias else None
+    check_weights(z, bias, 4, TYPES[dtype], sigmoid=sigmoid, renorm=True, **groups)
+
+
 def test_sums_of_two_best_beyond_32_bits():
     z = torch.randn(40, 16, generator=torch.Generator().manual_seed(9))
     bias = torch.tensor([3.0e38, 3.0e38, 0, 0, 3.1e38, 3.1e38, 0, 0, 3.3e38, 2.7e38, 0, 0, 3.2e38, 3.2e38, 0, 0])
