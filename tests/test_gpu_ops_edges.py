@@ -214,6 +214,39 @@ def test_large_scales_of_sums_that_are_0(M, K, N, counts):
     assert out[1::2, 1::2].isfinite().all() and (out[1::2, 1::2] != 0).all()
 
 
+FORMS = [
+    # kernel, M, K, N, counts, swiglu, pitch: two teams with several steps each, in even and odd numbers; rows quantised in the product's launch
+    ("q8_panel_kernel<false, 2>", 100, 2304, 8300, None, False, None), ("q8_panel_kernel<false, 2>", 100, 1300, 8300, None, False, None),
+    ("q8_panel_kernel<false, 2>", 300, 5640, 5000, None, False, 5648), ("q8_panel_kernel<true, 2>", 70, 2304, 9000, None, True, None),
+    ("q8_panel_kernel<true, 2>", 70, 1300, 9000, None, True, None), ("q8_panel_kernel<true, 2>", 70, 1793, 9000, None, True, 1808),
+    ("q8_panel_kernel<false, 2>", 0, 3100, 1024, [10, 0, 15, 9, 10, 70, 0, 2], False, None), ("q8_panel_kernel<false, 1>", 0, 2560, 1024, [10] * 64 + [0, 130], False, None),
+    ("q8_panel_kernel<true, 1>", 0, 1088, 1408, [30, 0, 1, 64, 65, 7] * 9, True, None),
+    ("q8_stream_kernel<1, false, 1, 8, 2, true>", 2, 520, 256, None, False, None), ("q8_stream_kernel<1, false, 2, 4, 1, true>", 3, 136, 20000, None, False, None),
+    ("q8_stream_kernel<1, false, 2, 1, 1, true>", 4, 72, 66000, None, False, None), ("q8_stream_kernel<1, true, 2, 4, 1, true>", 1, 1000, 512, None, True, None),
+    ("q8_stream_kernel<1, true, 2, 1, 1, true>", 2, 320, 66000, None, True, None),
+]
+
+
+@pytest.mark.parametrize("form,M,K,N,counts,swiglu,pitch", FORMS, ids=[f"{i}-{f[0][3:].replace(' ', '')}" for i, f in enumerate(FORMS)])
+def test_forms_of_the_product(form, M, K, N, counts, swiglu, pitch):
+    gen = torch.Generator().manual_seed(K + N)
+    M = sum(counts) if counts else M
+    x = torch.randn(M, K, generator=gen).bfloat16()
+    for _ in range(3):      # the profiler loses a session's events now and then
+        with torch.profiler.profile(activities=[torch.profiler.ProfilerActivity.CUDA]) as prof:
+            check_product(gen, x, len(counts) if counts else 1, N, counts, None, 1, swiglu, "bf16", pad_o=2, pitch=pitch, magnitude=4 / K ** 0.5)
+        ran = [e.name for e in prof.events() if "q8_" in e.name and "kernel" in e.name]
+        if ran:
+            break
+    assert len(ran) == 1 and form in ran[0], ran
+
+
+def test_a_prompt_of_codes_that_cannot_be_read_in_place():
+    gen = torch.Generator().manual_seed(12)
+    check_product(gen, torch.randn(2100, 1001, generator=gen), 1, 300, out="f32", codes=True)
+    check_product(gen, torch.randn(1200, 196, generator=gen), 4, 130, [500, 0, 1, 690], out="bf16", codes=True, swiglu=True, magnitude=0.3)
+
+
 # ---- weighted sum --------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("d,pad", [(8, 0), (33, 3)])
