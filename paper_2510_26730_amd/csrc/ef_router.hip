@@ -489,7 +489,8 @@ __global__ __launch_bounds__(64 * NW, VT <= 16 ? 4 : 2) void router_kernel(Route
                 const float worst = row_min(kept ? value : __builtin_inff()), best = row_max(kept ? kMinusInf : value);
                 // a sum of two that passes 32 bits: the wave's tokens are decided in 64
                 const float inf = __builtin_inff();
-                near = worst - best <= margin || __any(fabsf(value) == inf && fabsf(b1) < inf && fabsf(b2) < inf);
+                near = worst - best <= margin;
+                if (__builtin_expect(__any(fabsf(value) == inf), 0)) near |= __any(fabsf(value) == inf && fabsf(b1) < inf && fabsf(b2) < inf);
             }
         }
         uint32_t key[VT];
@@ -544,17 +545,16 @@ __global__ __launch_bounds__(64 * NW, VT <= 16 ? 4 : 2) void router_kernel(Route
         int place = 0;
         static_for<1, 16>([&](auto o) { place += dpp<kRor + decltype(o)::value>(l < k ? (uint32_t)e : 1u << 16) < (uint32_t)e; });
         const float z = mine ? mine_rows[shape.at(e)] : kMinusInf;
-        const float low = expf(-fabsf(z));
-        float w = softmax ? (z == m ? top : expf(z - m) * top) : (z < 0.f ? low : 1.f) / (1.f + low);
+        const float depth = softmax ? z - m : z, x0 = expf(softmax ? depth : -fabsf(z));
+        float w = softmax ? (z == m ? top : x0 * top) : (z < 0.f ? x0 : 1.f) / (1.f + x0);
         if (a.r.renorm) {
-            const float depth = softmax ? z - m : z;
-            if (__any(mine && depth < kDeep)) {
+            if (__builtin_expect(__any(mine && depth < kDeep), 0)) {
                 // Scores that 32 bits do not hold, or in part, keep their quotients without their common factor exp(zc): zc the largest
                 // chosen logit (sigmoid: 0 unless all are negative).  What is 0 in 64 bits counts as 0.
                 const float most = row_max(z), zc = softmax ? most : min_of(most, 0.f);
                 const float x = z == most ? 1.f : expf((softmax ? z : min_of(z, 0.f)) - zc);
                 const bool none = z == kMinusInf || (softmax ? depth < -745.1332f : z <= -709.7827f);
-                w = none ? 0.f : softmax ? x : x / (1.f + low);
+                w = none ? 0.f : softmax ? x : x / (1.f + x0);
             }
             const float sum = row_sum(w);
             w = sum > 0.f ? w / sum : 0.f;
