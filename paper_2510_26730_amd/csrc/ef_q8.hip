@@ -134,7 +134,8 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(QuantArgs a) {
     }
 }
 
-// Any row: strides, alignments and lengths that the kernel above does not take.  A workgroup takes a row and reads it twice.
+// Any row: strides, alignments and lengths that the kernel above does not take.  A workgroup takes a row and reads it twice, an element per
+// lane: 8192 rows of 4097 bf16 36 us, 38 in 32 bits, from the caches, where 4104 bf16 take 18 in the kernel above.
 template <int TYPE>
 __global__ __launch_bounds__(256) void quant_any_kernel(QuantArgs a) {
     using T = typename Element<TYPE>::T;
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(256) void quant_any_kernel(QuantArgs a) {
     }
 }
 
-// codes into rows whose bytes from K to the next multiple of 64 are zero
+// codes into rows whose bytes from K to the next multiple of 64 are zero, a byte per lane: 8192 rows of 4100 28 us
 __global__ __launch_bounds__(256) void pad_rows_kernel(QuantArgs a) {
     const int8_t *x = static_cast<const int8_t *>(a.x) + (size_t)blockIdx.x * a.ldx;
     int8_t *out = a.codes + (size_t)blockIdx.x * a.ldc;
@@ -536,7 +537,7 @@ hipError_t launch_quant_rows(const QuantArgs &all, hipStream_t s) {
 
 // Whether the product quantises rows itself (p.a: the rows as they are): up to four rows, one matrix, aligned to 16 bytes, whose codes
 // fit LDS.  1 x 4096 x 4096: 6.4 us in one launch against 3 + 6 and the gap between two.  Not for groups, whose tiles need LDS for 16
-// rows each and run four instead of five to a compute unit: 32 tokens of 64 experts, first half, 74 against 4.6 + 64.5 us.
+// rows each and run four instead of five to a compute unit: 32 tokens of 64 experts, first half, 74 against 4.7 + 60.9 us.
 bool q8_product_quantises(const Q8Args &p) {
     const int per = p.a_type == EF_F32 ? 4 : 8;
     return p.a_type != EF_I8 && p.G == 1 && p.M <= 4 && p.K % per == 0 && p.lda % per == 0 && reinterpret_cast<size_t>(p.a) % 16 == 0 &&

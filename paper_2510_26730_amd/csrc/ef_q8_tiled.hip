@@ -19,7 +19,6 @@ namespace ef {
 
 namespace {
 
-typedef int int4v __attribute__((ext_vector_type(4)));
 typedef int int16v __attribute__((ext_vector_type(16)));
 
 constexpr int kStages = 4;
