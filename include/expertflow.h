@@ -601,7 +601,8 @@ typedef struct ef_router {
  * c (ties: lower expert), ascending; w = s[ids], over their sum if renorm, times scale.  Then the stable grouping
  * of the assignments a = t*k + j by expert, as ef_route: counts, offsets, perm, inv_perm.
  * Comparisons are those of the scores' real values: s and c are formed in 32 bits, and again in 64 where the
- * border of a choice lies within the error of 32.  A logit of -inf or NaN has score 0 and choice value -inf (its
+ * border of a choice lies within the error of 32 (without a bias and without sums of two the logits themselves are compared, whose
+ * order is that of the scores also where these meet at 0 or 1).  A logit of -inf or NaN has score 0 and choice value -inf (its
  * expert comes after every other of its token); a bias of NaN counts as -inf; logits of +inf share a softmax
  * evenly.  A token whose scores are all 0 has weights 0, and its ids by the same rules; scores are those of 64 bits, and
  * renormalised weights have the right quotients also where 32 bits would hold the scores as 0 (a sigmoid of -100).
